@@ -39,7 +39,40 @@ class Segment(ctypes.Structure):
 MASK_EXPORTS = ("rapid_mask_select", "rapid_mask_select_workspace_bytes", "rapid_mask_select_joint",
                 "rapid_mask_select_joint_workspace_bytes", "rapid_attn_joint_select",
                 "rapid_attn_joint_select_workspace_bytes", "rapid_mask_level_tau")
+LAYER_EXPORTS = ("rapid_linear", "rapid_linear_workspace_bytes", "rapid_norm_modulate", "rapid_rope_table", "rapid_qk_norm_rope",
+                 "rapid_rope")
 CACHE_EXPORTS = ("rapid_cache_store", "rapid_cache_reuse", "rapid_equivalent_steps", "rapid_reward")
+
+
+class Rows(ctypes.Structure):
+    """rapid_rows of include/rapid_layer.h."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride_b", ctypes.c_longlong), ("stride_n", ctypes.c_longlong)]
+
+
+class QkSegment(ctypes.Structure):
+    """rapid_qk_segment of include/rapid_layer.h."""
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("n", ctypes.c_int),
+                ("in_stride_b", ctypes.c_longlong), ("in_stride_h", ctypes.c_longlong), ("in_stride_n", ctypes.c_longlong),
+                ("out_stride_b", ctypes.c_longlong), ("out_stride_h", ctypes.c_longlong),
+                ("out_stride_n", ctypes.c_longlong)]
+
+
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu_tanh": 2}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+
+
+class RopeAxis(ctypes.Structure):
+    """rapid_rope_axis of include/rapid_layer.h: RopeAxis(dim, theta, scaling, factor, original_length, beta_fast, beta_slow),
+    scaling one of ROPE_SCALINGS."""
+    _fields_ = [("dim", ctypes.c_int), ("scaling", ctypes.c_int), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_length", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
+
+    def __init__(self, dim, theta=10000.0, scaling="none", factor=1.0, original_length=0.0, beta_fast=32.0, beta_slow=1.0):
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+        super().__init__(dim, ROPE_SCALINGS[scaling], theta, factor, original_length, beta_fast, beta_slow)
 
 
 class RapidAttnError(RuntimeError):
@@ -113,6 +146,19 @@ def library():
     lib.rapid_equivalent_steps.restype = ci
     lib.rapid_reward.argtypes = [cd, cd, cd, cd, ci]
     lib.rapid_reward.restype = cd
+    rows, ll = ctypes.POINTER(Rows), ctypes.c_longlong
+    lib.rapid_linear.argtypes = [rows, vp, ll, vp, rows, ci, vp, ll, rows, ci, ci, ci, ci, vp, sz, vp]
+    lib.rapid_linear.restype = ci
+    lib.rapid_linear_workspace_bytes.argtypes = [ll, ci, ci]
+    lib.rapid_linear_workspace_bytes.restype = sz
+    lib.rapid_norm_modulate.argtypes = [rows, rows, vp, ll, vp, ll, ci, ci, ci, cf, vp]
+    lib.rapid_norm_modulate.restype = ci
+    lib.rapid_rope_table.argtypes = [vp, ll, ci, ctypes.POINTER(RopeAxis), cd, vp, vp]
+    lib.rapid_rope_table.restype = ci
+    lib.rapid_qk_norm_rope.argtypes = [ctypes.POINTER(QkSegment), ci, ci, ci, ci, cf, vp, ll, ci, ci, vp]
+    lib.rapid_qk_norm_rope.restype = ci
+    lib.rapid_rope.argtypes = [ctypes.POINTER(QkSegment), ci, ci, ci, ci, vp, ll, ci, ci, vp]
+    lib.rapid_rope.restype = ci
     _lib = lib
     return lib
 
@@ -524,3 +570,195 @@ def rapid_attn_joint_select(segments, block=128, kv_len=None, kv_lens=None, text
         _kv_lens_ptr(kv_lens, B, q0.device), N if text_start is None else int(text_start), float(tau), float(scale),
         mask_ptr, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(q0)))
     return [seg[3] for seg in segments]
+
+
+# ---------------------------------------------------------------- a layer around its attention
+def _on_device(device, call):
+    """call(stream) with torch's current stream of `device`, which is made the current device meanwhile (the default stream's
+    handle names none)."""
+    import torch
+    if torch._C._cuda_getDevice() == device:
+        return call(torch._C._cuda_getCurrentRawStream(device))
+    with torch.cuda.device(device):
+        return call(torch._C._cuda_getCurrentRawStream(device))
+
+
+def _rows(name, t, device=None):
+    """(descriptor, B, n, width) of a bf16 tensor [B, n, width], or [n, width] (B = 1), with a contiguous last dimension"""
+    import torch
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() in (2, 3)
+            and (t.stride(-1) == 1 or t.shape[-1] == 1)):
+        raise TypeError(f"{name} must be a CUDA bfloat16 tensor [B,n,width] or [n,width] with a contiguous last dimension")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on another device")
+    B, (n, width) = (t.shape[0] if t.dim() == 3 else 1), t.shape[-2:]
+    return Rows(t.data_ptr(), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)), B, n, width
+
+
+def _vectors(name, t, B, width, device):
+    """(pointer, stride) of a bf16 tensor [B, width], or [width] (one for all samples), with a contiguous last dimension; None"""
+    import torch
+    if t is None:
+        return None, 0
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() in (1, 2)
+            and (t.stride(-1) == 1 or t.shape[-1] == 1)):
+        raise TypeError(f"{name} must be a CUDA bfloat16 tensor [B,width] or [width] with a contiguous last dimension")
+    if tuple(t.shape) not in ((B, width), (width,)) or t.get_device() != device:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != {(B, width)}, or another device")
+    return t.data_ptr(), t.stride(0) if t.dim() == 2 else 0
+
+
+def rapid_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(library().rapid_linear_workspace_bytes(M, N, K))
+
+
+def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residual=None, workspace=None):
+    """out <- residual + gate * act(x weight^T + bias).  x [B,n,K] (or [n,K]), out and residual [B,n,N]: CUDA bf16, last dimension
+    contiguous; weight [N,K]; bias [N]; gate [B,N] or [N]; activation "none", "silu" or "gelu_tanh".  residual may be out.
+    `workspace`: CUDA uint8 tensor of at least rapid_linear_workspace_bytes(B*n, N, K) bytes; allocated with torch if None.
+    Returns out."""
+    import torch
+    xr, B, n, K = _rows("x", x)
+    device = x.get_device()
+    outr, Bo, no, N = _rows("out", out, device)
+    if (Bo, no) != (B, n):
+        raise ValueError(f"out: {tuple(out.shape)} does not go with x: {tuple(x.shape)}")
+    if not (isinstance(weight, torch.Tensor) and weight.is_cuda and weight.dtype is torch.bfloat16 and weight.dim() == 2
+            and (weight.stride(1) == 1 or K == 1)):
+        raise TypeError("weight must be a CUDA bfloat16 tensor [N,K] with a contiguous last dimension")
+    if tuple(weight.shape) != (N, K) or weight.get_device() != device:
+        raise ValueError(f"weight: shape {tuple(weight.shape)} != {(N, K)}, or another device")
+    bias_ptr, _ = _vectors("bias", bias, 1, N, device)
+    gate_ptr, gate_stride = _vectors("gate", gate, B, N, device)
+    res = None
+    if residual is not None:
+        res, Br, nr, Nr = _rows("residual", residual, device)
+        if (Br, nr, Nr) != (B, n, N):
+            raise ValueError(f"residual: {tuple(residual.shape)} does not go with out: {tuple(out.shape)}")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    if workspace is None:
+        need = rapid_linear_workspace_bytes(B * n, N, K)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    elif not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()
+              and workspace.get_device() == device):
+        raise TypeError("workspace must be a contiguous CUDA tensor on x's device")
+    ws_ptr, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(_on_device(device, lambda stream: library().rapid_linear(
+        xr, weight.data_ptr(), weight.stride(0) if N > 1 else K, bias_ptr, outr, ACTIVATIONS[activation], gate_ptr, gate_stride, res,
+        B, n, N, K, ws_ptr, ws_bytes, stream)))
+    return out
+
+
+def rapid_norm_modulate(x, out, scale=None, shift=None, eps=1e-6):
+    """out <- (x - mean) / sqrt(variance + eps) * (1 + scale) + shift over the last dimension.  x, out [B,n,C] (or [n,C]): CUDA
+    bf16, last dimension contiguous; scale, shift [B,C] or [C], both or neither.  out may be x.  Returns out."""
+    xr, B, n, C = _rows("x", x)
+    device = x.get_device()
+    outr, *shape = _rows("out", out, device)
+    if shape != [B, n, C]:
+        raise ValueError(f"out: {tuple(out.shape)} does not go with x: {tuple(x.shape)}")
+    if (scale is None) != (shift is None):
+        raise ValueError("scale and shift: both or neither")
+    scale_ptr, scale_stride = _vectors("scale", scale, B, C, device)
+    shift_ptr, shift_stride = _vectors("shift", shift, B, C, device)
+    _check(_on_device(device, lambda stream: library().rapid_norm_modulate(
+        xr, outr, scale_ptr, scale_stride, shift_ptr, shift_stride, B, n, C, float(eps), stream)))
+    return out
+
+
+def rapid_rope_table(positions, axes, table, magnitude=1.0):
+    """table[..., i, :] <- magnitude * (cos, sin) of the angle of pair i at each position.  positions: CUDA int32
+    [..., len(axes)] contiguous; axes: sequence of RopeAxis; table: CUDA float32 [..., rot / 2, 2] contiguous, rot the sum of
+    the axes' dims.  Returns table."""
+    import torch
+    if not (isinstance(positions, torch.Tensor) and positions.is_cuda and positions.dtype == torch.int32
+            and positions.dim() >= 2 and positions.is_contiguous()):
+        raise TypeError("positions must be a contiguous CUDA int32 tensor [...,axes]")
+    if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.float32 and table.is_contiguous()
+            and table.dim() >= 3):
+        raise TypeError("table must be a contiguous CUDA float32 tensor [...,rot/2,2]")
+    axes = list(axes)
+    pairs = sum(int(a.dim) for a in axes) // 2
+    device = positions.get_device()
+    if table.get_device() != device:
+        raise ValueError("table is on another device")
+    if positions.shape[-1] != len(axes) or tuple(table.shape) != (*positions.shape[:-1], pairs, 2):
+        raise ValueError(f"positions {tuple(positions.shape)} and table {tuple(table.shape)} do not go with {len(axes)} axes of "
+                         f"{pairs} pairs")
+    tokens = positions.numel() // len(axes) if axes else 0
+    _check(_on_device(device, lambda stream: library().rapid_rope_table(
+        positions.data_ptr(), tokens, len(axes), (RopeAxis * max(len(axes), 1))(*axes), float(magnitude), table.data_ptr(), stream)))
+    return table
+
+
+def _qk_rows(segments, weights, table, layout):
+    """(descriptors, B, H, D, table pointer, table stride, rot, layout, device)"""
+    import torch
+    if len(segments) not in (1, 2):
+        raise ValueError("one or two segments")
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(ROPE_LAYOUTS)}")
+    descr = (QkSegment * len(segments))()
+    first = device = None
+    N = 0
+    for i, (q, k, q_out, k_out) in enumerate(segments):
+        for name, t in (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out)):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() == 4
+                    and t.stride(3) == 1):
+                raise TypeError(f"segment {i}: {name} must be a CUDA bfloat16 tensor [B,H,n,D] with contiguous D")
+            device = t.get_device() if device is None else device
+            if t.shape != q.shape or t.get_device() != device:
+                raise ValueError(f"segment {i}: {name} shape/device differs")
+        if k.stride() != q.stride() or k_out.stride() != q_out.stride():
+            raise ValueError(f"segment {i}: q and k, and q_out and k_out, must share their strides")
+        B, H, n, D = q.shape
+        first = first or (B, H, D)
+        if (B, H, D) != first:
+            raise ValueError("segments differ in B, H or D")
+        w = [None, None]
+        if weights is not None:
+            if len(weights) != len(segments):
+                raise ValueError("one pair of weights for each segment")
+            for j, t in enumerate(weights[i]):
+                if t is None:
+                    continue
+                if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.is_contiguous()):
+                    raise TypeError(f"segment {i}: weights must be contiguous CUDA bfloat16 tensors [D]")
+                if tuple(t.shape) != (D,) or t.get_device() != device:
+                    raise ValueError(f"segment {i}: weights must be [D] on the segments' device")
+                w[j] = t.data_ptr()
+        descr[i] = QkSegment(q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), *w, n, *q.stride()[:3],
+                             *q_out.stride()[:3])
+        N += n
+    B, H, D = first
+    if table is None:
+        return descr, B, H, D, None, 0, 0, ROPE_LAYOUTS[layout], device
+    if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype == torch.float32 and table.is_contiguous()
+            and table.dim() in (3, 4)):
+        raise TypeError("table must be a contiguous CUDA float32 tensor [N,rot/2,2] or [B,N,rot/2,2]")
+    pairs = table.shape[-2]
+    if tuple(table.shape) not in ((N, pairs, 2), (B, N, pairs, 2)) or table.get_device() != device:
+        raise ValueError(f"table: shape {tuple(table.shape)} does not go with {B} samples of {N} tokens, or another device")
+    return (descr, B, H, D, table.data_ptr(), table.stride(0) if table.dim() == 4 else 0, 2 * pairs, ROPE_LAYOUTS[layout], device)
+
+
+def rapid_qk_norm_rope(segments, weights=None, table=None, layout="interleaved", eps=1e-6):
+    """Norm of every head's queries and keys and their rotation by position, one pass.  `segments`: one or two (q, k, q_out,
+    k_out), each CUDA bf16 indexed [B, H, n, D] with a contiguous last dimension and any other strides; q and k share theirs,
+    q_out and k_out theirs; q_out may be q and k_out k.  weights: a (q_weight, k_weight) for each segment, [D] or None;
+    table: float32 [N, rot/2, 2] (rapid_rope_table) over the joint tokens, or [B, N, rot/2, 2], or None: the norm alone;
+    layout "interleaved" or "half".  Returns the outputs, (q_out, k_out) of one segment after the other."""
+    descr, B, H, D, table_ptr, table_stride, rot, lay, device = _qk_rows(segments, weights, table, layout)
+    _check(_on_device(device, lambda stream: library().rapid_qk_norm_rope(
+        descr, len(segments), B, H, D, float(eps), table_ptr, table_stride, rot, lay, stream)))
+    return [t for seg in segments for t in seg[2:]]
+
+
+def rapid_rope(segments, table, layout="interleaved"):
+    """The rotation of rapid_qk_norm_rope alone.  Returns the outputs."""
+    descr, B, H, D, table_ptr, table_stride, rot, lay, device = _qk_rows(segments, None, table, layout)
+    _check(_on_device(device, lambda stream: library().rapid_rope(
+        descr, len(segments), B, H, D, table_ptr, table_stride, rot, lay, stream)))
+    return [t for seg in segments for t in seg[2:]]
