@@ -3,16 +3,37 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "rapid_layer.h"
 
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.44269504088896340736f;
+
+template <int CTRL>
+__device__ __forceinline__ float moved(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// The sum over the wavefront, in every lane.
+__device__ __forceinline__ float sum_of_lanes(float v)
+{
+    v += moved<0xB1>(v);                               // lane ^ 1
+    v += moved<0x4E>(v);                               // lane ^ 2
+    v += moved<0x141>(v);                              // 7 - lane of every 8
+    v += moved<0x140>(v);                              // 15 - lane of every 16
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 
 struct LinearParams {
     const __bf16* x;
@@ -21,10 +42,12 @@ struct LinearParams {
     const __bf16* gate;
     const __bf16* residual;
     __bf16* y;
-    long long x_sb, x_sn, y_sb, y_sn, r_sb, r_sn, w_sn, g_sb;
+    long long x_sb, y_sb, r_sb, g_sb;
+    int x_sn, y_sn, r_sn, w_sn;
     int M, n, N, K;          // M rows in samples of n (n = M where samples make no difference)
     int activation;
-    bool wide;               // N and everything the epilogue touches can be taken four elements at a time
+    int pieces, pitch;       // a product in pieces along K: how many, and floats from row to row of their sums
+    float* partial;          // [pieces, M, pitch]
 };
 
 // The sample and row of row m.
@@ -43,91 +66,505 @@ __device__ __forceinline__ float activated(float z, int activation)
     return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * t));
 }
 
-// Outputs j0 .. j0 + 3 of row m from their sums: everything in fp32, rounded once.
-__device__ __forceinline__ void finish(const LinearParams& p, int m, int j0, f32x4 sum)
+// What the epilogue adds and multiplies, and writes, eight outputs at a time: rows of odd widths start anywhere, so these accesses
+// may be aligned to two bytes only (the memory pipeline takes them).
+typedef bf16x8 bf16x8_anywhere __attribute__((aligned(2)));
+typedef bf16x4 bf16x4_anywhere __attribute__((aligned(2)));
+
+// Outputs j .. j + 7 of a row, or as many as there are
+__device__ __forceinline__ bf16x8 eight_of(const __bf16* at, int j, int N)
 {
-    int b, r;
-    sample_of(p, m, b, r);
-    __bf16* y = p.y + b * p.y_sb + r * p.y_sn + j0;
-    const __bf16* gate = p.gate ? p.gate + b * p.g_sb + j0 : nullptr;
-    const __bf16* res = p.residual ? p.residual + b * p.r_sb + r * p.r_sn + j0 : nullptr;
-    if (p.wide) {
-        bf16x4 out;
-        if (p.bias) {
-            const bf16x4 c = *(const bf16x4*)(p.bias + j0);
+    if (j + 8 <= N) return *(const bf16x8_anywhere*)(at + j);
+    bf16x8 v = {};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] += (float)c[i];
-        }
+    for (int i = 0; i < 7; ++i)
+        if (j + i < N) v[i] = at[j + i];
+    return v;
+}
+__device__ __forceinline__ void store_eight(__bf16* at, int j, int N, bf16x8 v)
+{
+    if (j + 8 <= N) { *(bf16x8_anywhere*)(at + j) = v; return; }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = activated(sum[i], p.activation);
-        if (gate) {
-            const bf16x4 c = *(const bf16x4*)gate;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] *= (float)c[i];
-        }
-        if (res) {
-            const bf16x4 c = *(const bf16x4*)res;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] += (float)c[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = (__bf16)sum[i];
-        *(bf16x4*)y = out;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (j0 + i >= p.N) break;
-        float z = sum[i] + (p.bias ? (float)p.bias[j0 + i] : 0.f);
-        z = activated(z, p.activation);
-        if (gate) z *= (float)gate[i];
-        if (res) z += (float)res[i];
-        y[i] = (__bf16)z;
-    }
+    for (int i = 0; i < 7; ++i)
+        if (j + i < N) at[j + i] = v[i];
 }
 
-constexpr int TILE = 64, STEP = 32, PITCH = STEP + 8;
-
-// 64 x 64 outputs per workgroup, 32 x 32 per wavefront, the operands staged through registers into LDS.  The product is computed
-// transposed (A = rows of w, B = rows of x), so that a lane holds four consecutive outputs of one row.
-__global__ __launch_bounds__(256) void linear_kernel(LinearParams p)
+// residual + gate * act(sum), everything in fp32, rounded once.  (What is not there is skipped by scalar branches.)
+__device__ __forceinline__ bf16x8 finished(const LinearParams& p, float (&z)[8], bf16x8 gate, bf16x8 residual)
 {
-    __shared__ __align__(16) __bf16 xs[TILE * PITCH], ws[TILE * PITCH];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int m0 = blockIdx.x * TILE, j0 = blockIdx.y * TILE;
-    const int row = tid >> 2, chunk = tid & 3;
-    int b, r;
-    sample_of(p, min(m0 + row, p.M - 1), b, r);
-    const __bf16* xr = p.x + b * p.x_sb + r * p.x_sn;
-    const __bf16* wr = p.w + (long long)min(j0 + row, p.N - 1) * p.w_sn;
-    f32x4 acc[2][2] = {};
-    for (int k0 = 0; k0 < p.K; k0 += STEP) {
-        const int k = k0 + 8 * chunk;
-        const u32x4 none = {0u, 0u, 0u, 0u};
-        const u32x4 xv = k < p.K ? *(const u32x4*)(xr + k) : none;
-        const u32x4 wv = k < p.K ? *(const u32x4*)(wr + k) : none;
-        __syncthreads();
-        *(u32x4*)(xs + row * PITCH + 8 * chunk) = xv;
-        *(u32x4*)(ws + row * PITCH + 8 * chunk) = wv;
-        __syncthreads();
-        bf16x8 a[2], c[2];
+    if (p.activation != RAPID_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            a[i] = *(const bf16x8*)(ws + ((wave & 1) * 32 + i * 16 + (lane & 15)) * PITCH + 8 * (lane >> 4));
-            c[i] = *(const bf16x8*)(xs + ((wave >> 1) * 32 + i * 16 + (lane & 15)) * PITCH + 8 * (lane >> 4));
+        for (int i = 0; i < 8; ++i) z[i] = activated(z[i], p.activation);
+    }
+    if (p.gate) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= (float)gate[i];
+    }
+    if (p.residual) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += (float)residual[i];
+    }
+    bf16x8 out;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = (__bf16)z[i];
+    return out;
+}
+
+// ---------------------------------------------------------------------------
+// Large products: 256 x 32*FN outputs per workgroup of 8 wavefronts (4 along the rows of x, 2 along those of w; a wavefront has
+// 64 x 16*FN), 64 inputs per step.
+// ---------------------------------------------------------------------------
+constexpr int STEP = 64;                               // inputs per step: 128 bytes of a row
+constexpr int ROW = STEP * 2;
+constexpr int CUS = 256;
+constexpr unsigned NOWHERE = 0xC0000000u;              // an offset outside any buffer below
+constexpr unsigned BUFFER = 0x80000100u;               // bytes that a tile's rows may span
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+
+// 1 KB from 64 lanes' addresses into LDS: lane i's 16 bytes go to dst + 16 i.  Assembly, so that only the waits below order it
+// (a wait state between the scalar write of M0 and the copy).
+__device__ __forceinline__ void copy_1k(unsigned long long base, int records, unsigned off, unsigned dst)
+{
+    const i32x4 rsrc = {(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), records, 0x00020000};
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(rsrc));
+}
+
+// s_waitcnt vmcnt(VM) lgkmcnt(0), then the barrier; nothing moves across.
+template <int VM>
+__device__ __forceinline__ void arrive()
+{
+    static_assert(VM >= 0 && VM < 64, "vmcnt is a 6-bit counter");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070 | (VM & 15) | ((VM >> 4) << 14));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Workgroups go to the XCDs in turn; every XCD gets a run of consecutive items.
+__device__ __forceinline__ int turn_of(int id, int items)
+{
+    constexpr int XCDS = 8;
+    const int x = id % XCDS, each = items / XCDS, more = items % XCDS;
+    return x * each + min(x, more) + id / XCDS;
+}
+// Consecutive tiles: GROUP of them along the rows of x, then along the rows of w, so that what an L2 holds is used by many.
+__device__ __forceinline__ void tile_of(int t, int mt, int nt, int& m, int& n)
+{
+    constexpr int GROUP = 4;
+    const int run = t / (GROUP * nt), in = t - run * GROUP * nt, rows = min(GROUP, mt - run * GROUP);
+    n = in / rows;
+    m = run * GROUP + in - n * rows;
+}
+
+template <int WR, int FN, bool SPLIT>
+__global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p, int items)
+{
+    constexpr int FM = 4, TM = 64 * WR, TN = 32 * FN, WAVES = 2 * WR;
+    constexpr int XB = TM * ROW, STAGE = XB + TN * ROW;               // bytes
+    constexpr int XC = TM / 8 / WAVES, WC = TN / 8 / WAVES, WREST = TN / 8 % WAVES;    // copies of a wavefront: of x; of w, and one more for some
+    constexpr int COPIES = XC + WC + (WREST ? 1 : 0);
+    __shared__ __align__(1024) char lds[2 * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool one = p.n == p.M;
+    const int wfirst = wave * WC + min(wave, WREST);                  // copies of w: WC + 1 of the first WREST wavefronts
+    const int mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN, all_steps = (p.K + STEP - 1) / STEP;
+
+    // Where the tile's copies come from.  Its first sample is the base of its x rows (its first row where there is one sample).
+    int m0, j0, b0, piece = 0, first = 0, steps = max(all_steps, 2);
+    unsigned long long xbase, wbase;
+    unsigned xoff[XC], woff[WC + 1];
+    auto locate = [&](int id) {
+        int mi, ni, t = turn_of(id, items);
+        if constexpr (SPLIT) {
+            piece = __builtin_amdgcn_readfirstlane(t / (mt * nt));
+            t -= piece * mt * nt;
+            first = __builtin_amdgcn_readfirstlane(piece * all_steps / p.pieces);
+            steps = max(__builtin_amdgcn_readfirstlane((piece + 1) * all_steps / p.pieces) - first, 2);
+        }
+        tile_of(t, mt, nt, mi, ni);
+        m0 = __builtin_amdgcn_readfirstlane(mi) * TM;
+        j0 = __builtin_amdgcn_readfirstlane(ni) * TN;
+    };
+    // (The lane's number, such that nothing made from it is kept in registers over the loops.)
+    auto lane_here = [&] {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    auto sources = [&] {
+        int r0;
+        const int lane = lane_here();
+        const unsigned chunk = (unsigned)((lane & 7) ^ (lane >> 3));  // the row's 16 bytes that this lane fetches, of every copy
+        sample_of(p, m0, b0, r0);
+        b0 = __builtin_amdgcn_readfirstlane(b0);
+        r0 = __builtin_amdgcn_readfirstlane(r0);
+        xbase = (unsigned long long)(p.x + b0 * p.x_sb + (one ? (long long)r0 * p.x_sn : 0)) + first * ROW;
+        wbase = (unsigned long long)(p.w + (long long)j0 * p.w_sn) + first * ROW;
+#pragma unroll
+        for (int i = 0; i < XC; ++i) {
+            int b, r;
+            sample_of(p, min(m0 + (wave * XC + i) * 8 + (lane >> 3), p.M - 1), b, r);
+            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk * 16u;
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < WC + 1; ++i)
+            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk * 16u;
+    };
+    auto mask = [&](int step) {                        // zeros for what lies behind the rows' ends
+        const int left = p.K - (first + step) * STEP;
+        if (left >= STEP) return;
+        const int lane = lane_here();
+        if (((lane & 7) ^ (lane >> 3)) * 8 >= left) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], c[j], acc[i][j], 0, 0, 0);
+            for (int i = 0; i < XC; ++i) xoff[i] = NOWHERE;
+#pragma unroll
+            for (int i = 0; i < WC + 1; ++i) woff[i] = NOWHERE;
+        }
+    };
+    int records = (int)BUFFER;
+    auto copy_one = [&](int stage, int c) {            // of x, then of w
+        const unsigned at = (unsigned)(size_t)(lds_char*)lds + (stage & 1) * STAGE;
+        if (c < XC) copy_1k(xbase, records, xoff[c], at + (wave * XC + c) * 1024);
+        else if (c < XC + WC || wave < WREST) copy_1k(wbase, records, woff[c - XC], at + XB + (wfirst + c - XC) * 1024);
+    };
+    auto copied = [&] {
+        xbase += ROW;
+        wbase += ROW;
+    };
+    auto copy = [&](int step, int stage) {
+        mask(step);
+#pragma unroll
+        for (int c = 0; c < COPIES; ++c) copy_one(stage, c);
+        copied();
+    };
+
+    // Fragments: lane (i, g) of 16 x 4 has row i's inputs 8 g .. 8 g + 7 of 32; the second half of a step is 64 bytes on.
+    const int wm = wave >> 1, wn = wave & 1;
+    const unsigned in_row = (unsigned)((lane & 15) * ROW + (((lane >> 4) ^ (lane & 7)) << 4));
+    const unsigned xat = in_row + wm * (16 * FM * ROW), wat = in_row + XB + wn * (16 * FN * ROW);
+    bf16x8 xf[2][FM], wf[2][FN];
+    auto fetch_one = [&](int stage, int half, int r, bf16x8 (&x)[FM], bf16x8 (&w)[FN]) {
+        lds_char* base = (lds_char*)lds + (stage & 1) * STAGE;
+        if (r < FM) x[r] = *(lds_bf16x8*)(base + (xat ^ (half * 64)) + r * 16 * ROW);
+        else w[r - FM] = *(lds_bf16x8*)(base + (wat ^ (half * 64)) + (r - FM) * 16 * ROW);
+    };
+    f32x4 acc[FN][FM];
+    // Half a step: FN blocks of FM MFMAs, each behind its share of the reads for the next half and of the copies for the step
+    // after the next.
+    auto half_step = [&](const bf16x8 (&x)[FM], const bf16x8 (&w)[FN], auto&& read, auto&& put) {
+        constexpr int READS = FM + FN, FIRST = FN > 2 ? FN - 2 : 1;          // the last blocks' MFMAs cover the last reads
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+#pragma unroll
+            for (int r = i * READS / FIRST; r < (i + 1) * READS / FIRST && r < READS; ++r) read(r);
+#pragma unroll
+            for (int c = i * COPIES / FN; c < (i + 1) * COPIES / FN; ++c) put(c);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i], x[j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto first_half = [&](int stage) {
+        half_step(xf[0], wf[0], [&](int r) { fetch_one(stage, 1, r, xf[1], wf[1]); }, [](int) {});
+        arrive<0>();                                   // everyone has read this step's tile, and the next one has arrived
+    };
+    auto second_half = [&](int stage, auto&& put) {
+        half_step(xf[1], wf[1], [&](int r) { fetch_one(stage + 1, 0, r, xf[0], wf[0]); }, put);
+        asm volatile("" ::: "memory");
+    };
+
+    // A lane's sums begin with the bias of its four columns of each fragment.
+    bf16x4 bias[FN] = {};
+    auto load_bias = [&] {
+        const int n = j0 + wn * 16 * FN + 4 * (lane_here() >> 4);
+        if (SPLIT || p.bias == nullptr) return;
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            if (j0 + TN <= p.N) {
+                bias[i] = *(const bf16x4_anywhere*)(p.bias + n + 16 * i);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) bias[i][q] = p.bias[min(n + 16 * i + q, p.N - 1)];
+            }
+        }
+    };
+
+    int id = blockIdx.x;
+    locate(id);
+    load_bias();
+    sources();
+    copy(0, 0);
+    copy(1, 1);
+    arrive<0>();
+    for (int stage = 0;;) {                            // stage of the tile's step s: stage + s
+#pragma unroll
+        for (int r = 0; r < FM + FN; ++r) fetch_one(stage, 0, r, xf[0], wf[0]);
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[i][j][q] = (float)bias[i][q];
+        const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_end = min(m0 + TM, p.M);
+        const bool more = id + (int)gridDim.x < items;
+        // The step two on is copied during the second half: behind the last steps the first two of this workgroup's next item, or
+        // nothing (a buffer without bytes).
+        for (int left = steps, next = 2; left > 0; --left, ++next, ++stage) {
+            if (left == 2) {
+                next = 0;
+                if (more) {
+                    id += gridDim.x;
+                    locate(id);
+                    sources();
+                } else records = 0;
+            }
+            mask(next);
+            first_half(stage);
+            second_half(stage, [&](int c) { copy_one(stage + 2, c); });
+            copied();
+        }
+
+        const int lane = lane_here();
+        if constexpr (SPLIT) {                         // this piece's sums, as they are
+            const int n = nw + 4 * (lane >> 4);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int m = mw + 16 * j + (lane & 15);
+                float* at = p.partial + ((long long)own_piece * p.M + m) * p.pitch + n;
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+                    if (m < p.M && n + 16 * i < p.pitch) *(f32x4*)(at + 16 * i) = acc[i][j];
+            }
+        } else {
+        // Pairs of fragments trade rows of lanes, so that a lane has eight consecutive outputs of a row: of (a, b) the lanes of
+        // rows 0, 2 get a's 0..7 and 8..15, those of rows 1, 3 b's.  Fragments side by side; of an odd number the last ones in
+        // pairs below each other.
+        const bool one_sample = one || tile_end <= (first_sample + 1) * p.n;
+        const int g = lane >> 4;
+        constexpr int SIDE = FN / 2, UNITS = FM * SIDE, ALL = UNITS + (FN % 2) * FM / 2;
+        auto of = [&](int m, const __bf16* t, long long sb, int sn) {       // row m of a tensor
+            int b = first_sample, r = m - first_sample * p.n;
+            if (!one_sample) sample_of(p, m, b, r);
+            return t + b * sb + (long long)r * sn;
+        };
+        auto row = [&](int u) { return mw + 16 * (u < UNITS ? u / SIDE : 2 * (u - UNITS) + (g & 1)) + (lane & 15); };
+        auto column = [&](int u) { return nw + (u < UNITS ? 32 * (u % SIDE) + (g & 1) * 16 : 16 * (FN - 1)) + (g >> 1) * 8; };
+        constexpr int AHEAD = ALL < 6 ? ALL : 6;       // residuals on their way
+        bf16x8 gate[SIDE + 1] = {}, residual[AHEAD] = {};
+        auto load_residual = [&](int u) {
+            if (p.residual && row(u) < p.M && column(u) < p.N)
+                residual[u % AHEAD] = eight_of(of(row(u), p.residual, p.r_sb, p.r_sn), column(u), p.N);
+        };
+        if (p.gate && one_sample) {
+#pragma unroll
+            for (int c = 0; c < SIDE + FN % 2; ++c) {
+                const int n = column(c < SIDE ? c : UNITS);
+                if (n < p.N) gate[c] = eight_of(p.gate + first_sample * p.g_sb, n, p.N);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load_residual(u);
+#pragma unroll
+        for (int u = 0; u < ALL; ++u) {
+            const int i = u < UNITS ? 2 * (u % SIDE) : FN - 1, j = u < UNITS ? u / SIDE : 2 * (u - UNITS);
+            const f32x4 a = acc[i][j], b = u < UNITS ? acc[i + 1][j] : acc[i][j + 1];
+            float z[8];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[q]), __float_as_uint(b[q]), false, false);
+                z[q] = __uint_as_float(both[0]);
+                z[4 + q] = __uint_as_float(both[1]);
+            }
+            const int m = row(u), n = column(u);
+            bf16x8 by = gate[u < UNITS ? u % SIDE : SIDE];
+            if (p.gate && !one_sample && m < p.M && n < p.N) by = eight_of(of(m, p.gate, p.g_sb, 0), n, p.N);
+            const bf16x8 out = finished(p, z, by, residual[u % AHEAD]);
+            if (u + AHEAD < ALL) load_residual(u + AHEAD);
+            if (u == ALL / 2 && more) load_bias();     // (half of the sums' registers are free)
+            if (m < p.M && n < p.N) store_eight((__bf16*)of(m, p.y, p.y_sb, p.y_sn), n, p.N, out);
+        }
+        }
+        if (!more) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies, of nothing, write zeros: not into another workgroup's LDS
+}
+
+// The sums of a product's pieces, in their order, and the epilogue: eight outputs a lane.
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
+{
+    const unsigned per_row = (unsigned)p.pitch / 8, at = blockIdx.x * 256 + threadIdx.x, m = at / per_row;
+    const int n = 8 * (int)(at - m * per_row);
+    if (m >= (unsigned)p.M || n >= p.N) return;
+    int b, r;
+    sample_of(p, (int)m, b, r);
+    bf16x8 bias = {}, gate = {}, residual = {};
+    if (p.bias) bias = eight_of(p.bias, n, p.N);
+    if (p.gate) gate = eight_of(p.gate + b * p.g_sb, n, p.N);
+    if (p.residual) residual = eight_of(p.residual + b * p.r_sb + (long long)r * p.r_sn, n, p.N);
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = (float)bias[i];
+    const float* from = p.partial + (long long)m * p.pitch + n;
+    for (int s = 0; s < p.pieces; ++s, from += (long long)p.M * p.pitch) {
+        const f32x4 a = *(const f32x4*)from, c = *(const f32x4*)(from + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { z[i] += a[i]; z[4 + i] += c[i]; }
+    }
+    store_eight(p.y + b * p.y_sb + (long long)r * p.y_sn, n, p.N, finished(p, z, gate, residual));
+}
+
+// ---------------------------------------------------------------------------
+// A handful of rows (the conditioning's projections): MAX_M of x at most.  A wavefront takes OUT outputs of all rows and reads their
+// rows of w end to end, 1 KB an access; two products an instruction, the lanes' sums are added at the end.
+// ---------------------------------------------------------------------------
+constexpr int OUT = 4, DOT_WAVES = 4, DOT_ROWS = 4;
+
+template <int MAX_M>
+__global__ __launch_bounds__(DOT_WAVES * 64) void linear_dot_kernel(LinearParams p)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j0 = (blockIdx.x * DOT_WAVES + wave) * OUT;
+    if (j0 >= p.N) return;
+    const __bf16 *x[MAX_M], *w[OUT];
+#pragma unroll
+    for (int m = 0; m < MAX_M; ++m) {
+        int b, r;
+        sample_of(p, min(m, p.M - 1), b, r);
+        x[m] = p.x + b * p.x_sb + (long long)r * p.x_sn;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < OUT; ++j) w[j] = p.w + (long long)min(j0 + j, p.N - 1) * p.w_sn;
+    float acc[OUT][MAX_M] = {};
+    auto some = [&](int k, auto count) {               // count times 512 inputs from k on
+        constexpr int COUNT = decltype(count)::value;
+        u32x4 wv[COUNT][OUT], xv[COUNT][MAX_M];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int m = m0 + (wave >> 1) * 32 + j * 16 + (lane & 15), n = j0 + (wave & 1) * 32 + i * 16 + 4 * (lane >> 4);
-            if (m < p.M && n < p.N) finish(p, m, n, acc[i][j]);
+        for (int c = 0; c < COUNT; ++c) {
+            const int at = k + 512 * c + 8 * lane;
+            const u32x4 none = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < OUT; ++j) wv[c][j] = COUNT > 1 || at < p.K ? *(const u32x4*)(w[j] + at) : none;
+#pragma unroll
+            for (int m = 0; m < MAX_M; ++m) xv[c][m] = COUNT > 1 || at < p.K ? *(const u32x4*)(x[m] + at) : none;
         }
+        __builtin_amdgcn_sched_barrier(0);             // all of them are on their way before the first product
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c)
+#pragma unroll
+            for (int j = 0; j < OUT; ++j)
+#pragma unroll
+                for (int m = 0; m < MAX_M; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const unsigned a = wv[c][j][i], b = xv[c][m][i];
+                        acc[j][m] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), acc[j][m], false);
+                    }
+    };
+    constexpr int AHEAD = 3;
+    int k = 0;
+    for (; k + 512 * AHEAD <= p.K; k += 512 * AHEAD) some(k, std::integral_constant<int, AHEAD>());
+    for (; k < p.K; k += 512) some(k, std::integral_constant<int, 1>());
+    // lane j * MAX_M + m keeps the sum of output j of row m
+    float mine = 0.f;
+#pragma unroll
+    for (int j = 0; j < OUT; ++j)
+#pragma unroll
+        for (int m = 0; m < MAX_M; ++m) {
+            const float sum = sum_of_lanes(acc[j][m]);
+            mine = lane == j * MAX_M + m ? sum : mine;
+        }
+    const int j = lane / MAX_M, m = lane - j * MAX_M, n = j0 + j;
+    if (j >= OUT || m >= p.M || n >= p.N) return;
+    int b, r;
+    sample_of(p, m, b, r);
+    if (p.bias) mine += (float)p.bias[n];
+    mine = activated(mine, p.activation);
+    if (p.gate) mine *= (float)p.gate[b * p.g_sb + n];
+    if (p.residual) mine += (float)p.residual[b * p.r_sb + (long long)r * p.r_sn + n];
+    p.y[b * p.y_sb + (long long)r * p.y_sn + n] = (__bf16)mine;
+}
+
+template <int MAX_M>
+int launch_dot(const LinearParams& p, void* stream)
+{
+    constexpr int EACH = OUT * DOT_WAVES;
+    hipLaunchKernelGGL((linear_dot_kernel<MAX_M>), dim3((unsigned)((p.N + EACH - 1) / EACH)), dim3(DOT_WAVES * 64), 0, (hipStream_t)stream, p);
+    return hipGetLastError() == hipSuccess ? RAPID_OK : RAPID_ERR_DEVICE;
+}
+
+template <int WR, int FN, bool SPLIT>
+int launch_wide(const LinearParams& p, void* stream)
+{
+    constexpr int TM = 64 * WR, TN = 32 * FN;
+    const long long items = (((long long)p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * (SPLIT ? p.pieces : 1);
+    if (items >= (1LL << 31) - 4096) return RAPID_ERR_SHAPE;
+    const long long most = CUS * (4 / WR);
+    hipLaunchKernelGGL((linear_wide_kernel<WR, FN, SPLIT>), dim3((unsigned)(items < most ? items : most)), dim3(WR * 128), 0,
+                       (hipStream_t)stream, p, (int)items);
+    if constexpr (SPLIT) {
+        const long long lanes = (long long)p.M * (p.pitch / 8);
+        hipLaunchKernelGGL(linear_join_kernel, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, (hipStream_t)stream, p);
+    }
+    return hipGetLastError() == hipSuccess ? RAPID_OK : RAPID_ERR_DEVICE;
+}
+
+// ---------------------------------------------------------------------------
+// Which tile, and how many pieces along K
+// ---------------------------------------------------------------------------
+enum Tile { T64x64, T128x128, T256x160, T256x192, T256x256, TILES };
+struct Plan {
+    Tile tile;
+    int pieces;
+};
+constexpr int MOST_PIECES = 8;
+
+// What a product takes, in us.  Its items (tiles times pieces) go to 256 CUs with each slots of them at a time: full rounds, whose
+// steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full`; every round
+// has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.  Pieces are added up by a second kernel,
+// which costs `join` and `sum` for every million numbers that it reads.  Fitted to 600 products of 5 to 32768 rows, 16 to 9728
+// outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8 pieces: the plan found by it takes 1.023 times
+// what the best one does in the geometric mean (1.38 times at most, where few outputs meet many rows).
+struct TileCost {
+    int rows, columns, slots;
+    float alone, full, ends, odd, call, join, sum;
+};
+constexpr TileCost COST[TILES] = {
+    {64, 64, 4, 0.252f, 0.890f, 1.78f, 0.44f, 2.73f, 2.23f, 2.17f}, {128, 128, 2, 0.402f, 1.130f, 3.32f, 0.67f, 2.32f, 1.95f, 1.53f},
+    {256, 160, 1, 0.692f, 1.242f, 4.42f, 0.73f, 2.05f, 0.f, 0.f},   {256, 192, 1, 0.752f, 1.374f, 4.94f, 0.81f, 2.14f, 0.f, 0.f},
+    {256, 256, 1, 0.949f, 1.672f, 6.48f, 0.83f, 1.86f, 0.f, 0.f}};
+
+float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
+{
+    const long long items = ((M + c.rows - 1) / c.rows) * ((N + c.columns - 1) / c.columns) * pieces, slots = CUS * c.slots;
+    const int all = (K + STEP - 1) / STEP;
+    const float steps = all > 2 ? (float)all / pieces : 2.f, load = (float)(items % slots) / CUS;
+    const float ends = N % 8 != 0 && pieces == 1 ? c.ends + c.odd : c.ends;
+    float t = c.call + (float)(items / slots) * (steps * c.full + ends);
+    if (items % slots != 0) {
+        const float crowd = c.slots == 1 ? load : load > 1.f ? (load - 1.f) / (c.slots - 1) : 0.f;
+        t += steps * (c.alone + (c.full - c.alone) * crowd) + ends;
+    }
+    return pieces > 1 ? t + c.join + c.sum * 1e-6f * (float)M * (float)N * pieces : t;
+}
+
+Plan plan_for(long long M, int N, int K, int most_pieces)
+{
+    Plan best = {T64x64, 1};
+    float least = cost_of(COST[T64x64], M, N, K, 1);
+    for (int t = 0; t < TILES; ++t) {
+        // (a piece has two steps at least; larger tiles have work enough, or few steps)
+        const int most = t <= T128x128 ? most_pieces : 1;
+        for (int pieces = 1; pieces <= most && (pieces == 1 || 2 * pieces * STEP <= K); ++pieces) {
+            const float c = cost_of(COST[t], M, N, K, pieces);
+            if (c < least) { least = c; best = {(Tile)t, pieces}; }
+        }
+    }
+    return best;
 }
 
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -135,10 +572,11 @@ inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintp
 constexpr long long MAX_STRIDE = 1LL << 22;            // elements, of a row
 
 // Strides of dimensions of size 1 replaced by what changes no address; false: out of range.
-bool rows_ok(const rapid_rows& a, int B, int n, int width, bool written, long long& sb, long long& sn)
+bool rows_ok(const rapid_rows& a, int B, int n, int width, bool written, long long& sb, int& row_stride)
 {
-    sn = n == 1 ? width : a.stride_n;
+    const long long sn = n == 1 ? width : a.stride_n;
     sb = B == 1 ? 0 : a.stride_b;
+    row_stride = (int)sn;
     if (sn < 0 || sn > MAX_STRIDE || sb < 0 || sb > (1LL << 40)) return false;
     if (!written) return true;
     // apart: rows behind each other and samples behind each other, or samples within the rows' distance
@@ -147,16 +585,15 @@ bool rows_ok(const rapid_rows& a, int B, int n, int width, bool written, long lo
     return n > 1 ? sn >= width : B == 1 || sb >= width;
 }
 
-inline bool by_four(const void* p, long long sb, long long sn) { return p == nullptr || (aligned(p, 8) && sb % 4 == 0 && sn % 4 == 0); }
-
 }  // namespace
 
 extern "C" {
 
 size_t rapid_linear_workspace_bytes(long long M, int N, int K)
 {
-    (void)M; (void)N; (void)K;
-    return 0;
+    if (M <= DOT_ROWS || M >= (1LL << 31) - 256 || N <= 0 || N > MAX_STRIDE || K <= 0 || K > MAX_STRIDE || K % 8 != 0) return 0;
+    const int pieces = plan_for(M, N, K, MOST_PIECES).pieces;
+    return pieces > 1 ? (size_t)pieces * M * ((N + 7) / 8 * 8) * sizeof(float) : 0;
 }
 
 int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const void* bias, const rapid_rows* y, int activation,
@@ -177,9 +614,9 @@ int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const v
     if (!aligned(x->ptr, 16) || !aligned(w, 16) || p.x_sb % 8 != 0 || p.x_sn % 8 != 0 || w_stride % 8 != 0) return RAPID_ERR_ALIGN;
     if (!aligned(y->ptr, 2) || !aligned(bias, 2) || !aligned(gate, 2) || (residual && !aligned(residual->ptr, 2))) return RAPID_ERR_ALIGN;
     // rows of one tile are addressed from its first sample by 32 bits
-    if (B > 1 && (255 / n + 1) * p.x_sb + (n - 1) * p.x_sn + K > (1LL << 30)) return RAPID_ERR_SHAPE;
+    if (B > 1 && (255 / n + 1) * p.x_sb + (long long)(n - 1) * p.x_sn + K > (1LL << 30)) return RAPID_ERR_SHAPE;
     if (y->ptr == x->ptr || y->ptr == w) return RAPID_ERR_ALIAS;
-    const size_t need = rapid_linear_workspace_bytes(M, N, K);
+    const size_t need = workspace ? rapid_linear_workspace_bytes(M, N, K) : 0;
     if (workspace && (workspace_bytes < need || !aligned(workspace, 16))) return RAPID_ERR_WORKSPACE;
     p.x = (const __bf16*)x->ptr;
     p.w = (const __bf16*)w;
@@ -187,20 +624,27 @@ int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const v
     p.gate = (const __bf16*)gate;
     p.residual = residual ? (const __bf16*)residual->ptr : nullptr;
     p.y = (__bf16*)y->ptr;
-    p.w_sn = w_stride;
+    p.w_sn = (int)w_stride;
     p.g_sb = gs;
     p.M = (int)M;
     p.n = n;
     p.N = N;
     p.K = K;
     p.activation = activation;
-    p.wide = N % 4 == 0 && by_four(p.bias, 0, 0) && by_four(p.gate, p.g_sb, 0) && by_four(p.residual, p.r_sb, p.r_sn) &&
-             by_four(p.y, p.y_sb, p.y_sn);
     if (B == 1) p.n = p.M;
-    const long long mt = (M + TILE - 1) / TILE, nt = (N + TILE - 1) / TILE;
-    if (nt > 65535) return RAPID_ERR_SHAPE;
-    hipLaunchKernelGGL(linear_kernel, dim3((unsigned)mt, (unsigned)nt), dim3(256), 0, (hipStream_t)stream, p);
-    return hipGetLastError() == hipSuccess ? RAPID_OK : RAPID_ERR_DEVICE;
+    if (M <= DOT_ROWS) return M == 1 ? launch_dot<1>(p, stream) : M == 2 ? launch_dot<2>(p, stream) : launch_dot<4>(p, stream);
+    const Plan plan = plan_for(M, N, K, workspace ? MOST_PIECES : 1);
+    p.pieces = plan.pieces;
+    p.pitch = (N + 7) / 8 * 8;
+    p.partial = (float*)workspace;
+    if (plan.pieces > 1) return plan.tile == T64x64 ? launch_wide<1, 2, true>(p, stream) : launch_wide<2, 4, true>(p, stream);
+    switch (plan.tile) {
+    case T64x64: return launch_wide<1, 2, false>(p, stream);
+    case T128x128: return launch_wide<2, 4, false>(p, stream);
+    case T256x160: return launch_wide<4, 5, false>(p, stream);
+    case T256x192: return launch_wide<4, 6, false>(p, stream);
+    default: return launch_wide<4, 8, false>(p, stream);
+    }
 }
 
 }  // extern "C"
