@@ -164,27 +164,36 @@ __device__ __forceinline__ void tile_of(int t, int mt, int nt, int& m, int& n)
 template <int WR, int FN, bool SPLIT>
 __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p, int items)
 {
-    constexpr int FM = 4, TM = 64 * WR, TN = 32 * FN, WAVES = 2 * WR;
-    constexpr int XB = TM * ROW, STAGE = XB + TN * ROW;               // bytes
+    constexpr int FM = 4, TM = 64 * WR, TN = 32 * FN, WAVES = 2 * WR, PER_CU = 4 / WR;
+    constexpr int XB = TM * ROW, WB = TN * ROW;                       // bytes of a step
+    // Steps in LDS: three of both operands where they fit, else of the one that comes from further away: x where tiles are large
+    // (many rows; all of them use w at the same time), w where they are small.
+    constexpr bool BOTH = 3 * (XB + WB) <= 160 * 1024 / PER_CU;
+    constexpr int XS = BOTH || WR == 4 ? 3 : 2, WS = BOTH || WR < 4 ? 3 : 2, MOST = 3;
+    static_assert(XS * XB + WS * WB <= 160 * 1024 / PER_CU, "");
     constexpr int XC = TM / 8 / WAVES, WC = TN / 8 / WAVES, WREST = TN / 8 % WAVES;    // copies of a wavefront: of x; of w, and one more for some
-    constexpr int COPIES = XC + WC + (WREST ? 1 : 0);
-    __shared__ __align__(1024) char lds[2 * STAGE];
+    constexpr int WALL = WC + (WREST ? 1 : 0), COPIES = XC + WALL;
+    constexpr int LATE = BOTH ? XC + WC : XS > WS ? XC : WC;          // copies that may be on their way yet when a step begins
+    __shared__ __align__(1024) char lds[XS * XB + WS * WB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool one = p.n == p.M;
     const int wfirst = wave * WC + min(wave, WREST);                  // copies of w: WC + 1 of the first WREST wavefronts
     const int mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN, all_steps = (p.K + STEP - 1) / STEP;
 
     // Where the tile's copies come from.  Its first sample is the base of its x rows (its first row where there is one sample).
-    int m0, j0, b0, piece = 0, first = 0, steps = max(all_steps, 2);
+    int m0, j0, b0, piece = 0, first = 0, steps = max(all_steps, MOST), xplace, wplace;
+    // Rows lie a multiple of many memory channels apart, so the same step of all of them lies in few channels: every XCD begins
+    // at another step and comes round to those before it (its workgroups stay together, they share what its L2 holds).
+    const int turn = !SPLIT && all_steps >= 8 && p.K % STEP == 0 ? (int)(blockIdx.x % 8) * all_steps / 8 : 0;
     unsigned long long xbase, wbase;
-    unsigned xoff[XC], woff[WC + 1];
+    unsigned xoff[XC], woff[WALL];
     auto locate = [&](int id) {
         int mi, ni, t = turn_of(id, items);
         if constexpr (SPLIT) {
             piece = __builtin_amdgcn_readfirstlane(t / (mt * nt));
             t -= piece * mt * nt;
             first = __builtin_amdgcn_readfirstlane(piece * all_steps / p.pieces);
-            steps = max(__builtin_amdgcn_readfirstlane((piece + 1) * all_steps / p.pieces) - first, 2);
+            steps = max(__builtin_amdgcn_readfirstlane((piece + 1) * all_steps / p.pieces) - first, MOST);
         }
         tile_of(t, mt, nt, mi, ni);
         m0 = __builtin_amdgcn_readfirstlane(mi) * TM;
@@ -196,66 +205,59 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         asm volatile("" : "+v"(l));
         return l;
     };
-    auto sources = [&] {
+    auto chunk_of = [](int lane) { return (unsigned)((lane & 7) ^ (lane >> 3)); };    // the row's 16 bytes that a lane fetches
+    auto sources_x = [&] {
         int r0;
         const int lane = lane_here();
-        const unsigned chunk = (unsigned)((lane & 7) ^ (lane >> 3));  // the row's 16 bytes that this lane fetches, of every copy
         sample_of(p, m0, b0, r0);
         b0 = __builtin_amdgcn_readfirstlane(b0);
         r0 = __builtin_amdgcn_readfirstlane(r0);
-        xbase = (unsigned long long)(p.x + b0 * p.x_sb + (one ? (long long)r0 * p.x_sn : 0)) + first * ROW;
-        wbase = (unsigned long long)(p.w + (long long)j0 * p.w_sn) + first * ROW;
+        xbase = (unsigned long long)(p.x + b0 * p.x_sb + (one ? (long long)r0 * p.x_sn : 0)) + (first + turn) * ROW;
+        xplace = turn;
 #pragma unroll
         for (int i = 0; i < XC; ++i) {
             int b, r;
             sample_of(p, min(m0 + (wave * XC + i) * 8 + (lane >> 3), p.M - 1), b, r);
-            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk * 16u;
+            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk_of(lane) * 16u;
         }
-#pragma unroll
-        for (int i = 0; i < WC + 1; ++i)
-            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk * 16u;
     };
-    auto mask = [&](int step) {                        // zeros for what lies behind the rows' ends
+    auto sources_w = [&] {
+        const int lane = lane_here();
+        wbase = (unsigned long long)(p.w + (long long)j0 * p.w_sn) + (first + turn) * ROW;
+        wplace = turn;
+#pragma unroll
+        for (int i = 0; i < WALL; ++i)
+            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk_of(lane) * 16u;
+    };
+    auto mask = [&](int step, auto& off) {             // zeros for what lies behind the rows' ends
         const int left = p.K - (first + step) * STEP;
         if (left >= STEP) return;
-        const int lane = lane_here();
-        if (((lane & 7) ^ (lane >> 3)) * 8 >= left) {
-#pragma unroll
-            for (int i = 0; i < XC; ++i) xoff[i] = NOWHERE;
-#pragma unroll
-            for (int i = 0; i < WC + 1; ++i) woff[i] = NOWHERE;
-        }
+        if ((int)chunk_of(lane_here()) * 8 >= left)
+            for (unsigned& o : off) o = NOWHERE;
     };
-    int records = (int)BUFFER;
-    auto copy_one = [&](int stage, int c) {            // of x, then of w
-        const unsigned at = (unsigned)(size_t)(lds_char*)lds + (stage & 1) * STAGE;
-        if (c < XC) copy_1k(xbase, records, xoff[c], at + (wave * XC + c) * 1024);
-        else if (c < XC + WC || wave < WREST) copy_1k(wbase, records, woff[c - XC], at + XB + (wfirst + c - XC) * 1024);
+    int xrecords = (int)BUFFER, wrecords = (int)BUFFER;
+    auto copy_x = [&](int slot, int c) { copy_1k(xbase, xrecords, xoff[c], (unsigned)(size_t)(lds_char*)lds + slot * XB + (wave * XC + c) * 1024); };
+    auto copy_w = [&](int slot, int c) {
+        if (c < WC || wave < WREST) copy_1k(wbase, wrecords, woff[c], (unsigned)(size_t)(lds_char*)lds + XS * XB + slot * WB + (wfirst + c) * 1024);
     };
-    auto copied = [&] {
-        xbase += ROW;
-        wbase += ROW;
-    };
-    auto copy = [&](int step, int stage) {
-        mask(step);
-#pragma unroll
-        for (int c = 0; c < COPIES; ++c) copy_one(stage, c);
-        copied();
+    auto on = [&](unsigned long long& base, int& place) {
+        const bool round = ++place == steps;
+        base += round ? ROW - steps * ROW : ROW;
+        place = round ? 0 : place;
     };
 
     // Fragments: lane (i, g) of 16 x 4 has row i's inputs 8 g .. 8 g + 7 of 32; the second half of a step is 64 bytes on.
     const int wm = wave >> 1, wn = wave & 1;
     const unsigned in_row = (unsigned)((lane & 15) * ROW + (((lane >> 4) ^ (lane & 7)) << 4));
-    const unsigned xat = in_row + wm * (16 * FM * ROW), wat = in_row + XB + wn * (16 * FN * ROW);
+    const unsigned xat = in_row + wm * (16 * FM * ROW), wat = in_row + XS * XB + wn * (16 * FN * ROW);
     bf16x8 xf[2][FM], wf[2][FN];
-    auto fetch_one = [&](int stage, int half, int r, bf16x8 (&x)[FM], bf16x8 (&w)[FN]) {
-        lds_char* base = (lds_char*)lds + (stage & 1) * STAGE;
-        if (r < FM) x[r] = *(lds_bf16x8*)(base + (xat ^ (half * 64)) + r * 16 * ROW);
-        else w[r - FM] = *(lds_bf16x8*)(base + (wat ^ (half * 64)) + (r - FM) * 16 * ROW);
+    auto fetch_one = [&](int xslot, int wslot, int half, int r, bf16x8 (&x)[FM], bf16x8 (&w)[FN]) {
+        if (r < FM) x[r] = *(lds_bf16x8*)((lds_char*)lds + xslot * XB + (xat ^ (half * 64)) + r * 16 * ROW);
+        else w[r - FM] = *(lds_bf16x8*)((lds_char*)lds + wslot * WB + (wat ^ (half * 64)) + (r - FM) * 16 * ROW);
     };
     f32x4 acc[FN][FM];
-    // Half a step: FN blocks of FM MFMAs, each behind its share of the reads for the next half and of the copies for the step
-    // after the next.
+    // Half a step: FN blocks of FM MFMAs, each behind its share of the reads for the next half and of the copies for a step
+    // to come.
     auto half_step = [&](const bf16x8 (&x)[FM], const bf16x8 (&w)[FN], auto&& read, auto&& put) {
         constexpr int READS = FM + FN, FIRST = FN > 2 ? FN - 2 : 1;          // the last blocks' MFMAs cover the last reads
 #pragma unroll
@@ -269,15 +271,6 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto first_half = [&](int stage) {
-        half_step(xf[0], wf[0], [&](int r) { fetch_one(stage, 1, r, xf[1], wf[1]); }, [](int) {});
-        arrive<0>();                                   // everyone has read this step's tile, and the next one has arrived
-    };
-    auto second_half = [&](int stage, auto&& put) {
-        half_step(xf[1], wf[1], [&](int r) { fetch_one(stage + 1, 0, r, xf[0], wf[0]); }, put);
-        asm volatile("" ::: "memory");
-    };
-
     // A lane's sums begin with the bias of its four columns of each fragment.
     bf16x4 bias[FN] = {};
     auto load_bias = [&] {
@@ -297,13 +290,27 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     int id = blockIdx.x;
     locate(id);
     load_bias();
-    sources();
-    copy(0, 0);
-    copy(1, 1);
-    arrive<0>();
-    for (int stage = 0;;) {                            // stage of the tile's step s: stage + s
+    sources_x();
+    sources_w();
 #pragma unroll
-        for (int r = 0; r < FM + FN; ++r) fetch_one(stage, 0, r, xf[0], wf[0]);
+    for (int i = 0; i < MOST; ++i) {
+        if (i < XS) {
+            mask(i, xoff);
+#pragma unroll
+            for (int c = 0; c < XC; ++c) copy_x(i, c);
+            on(xbase, xplace);
+        }
+        if (i < WS) {
+            mask(i, woff);
+#pragma unroll
+            for (int c = 0; c < WALL; ++c) copy_w(i, c);
+            on(wbase, wplace);
+        }
+    }
+    arrive<0>();
+    for (int xslot = 0, wslot = 0;;) {
+#pragma unroll
+        for (int r = 0; r < FM + FN; ++r) fetch_one(xslot, wslot, 0, r, xf[0], wf[0]);
 #pragma unroll
         for (int i = 0; i < FN; ++i)
 #pragma unroll
@@ -312,21 +319,41 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
                 for (int q = 0; q < 4; ++q) acc[i][j][q] = (float)bias[i][q];
         const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_end = min(m0 + TM, p.M);
         const bool more = id + (int)gridDim.x < items;
-        // The step two on is copied during the second half: behind the last steps the first two of this workgroup's next item, or
-        // nothing (a buffer without bytes).
-        for (int left = steps, next = 2; left > 0; --left, ++next, ++stage) {
-            if (left == 2) {
-                next = 0;
-                if (more) {
-                    id += gridDim.x;
-                    locate(id);
-                    sources();
-                } else records = 0;
+        const int length = steps;
+        // A step's buffer is free once its second half is in registers: the step XS (WS) on goes there during the multiplication of
+        // that half; behind the last steps the first ones of this workgroup's next item, or nothing (a buffer without bytes).
+        for (int left = steps, xnext = XS, wnext = WS; left > 0; --left, ++xnext, ++wnext) {
+            if (left == MOST && more) {
+                id += gridDim.x;
+                locate(id);
             }
-            mask(next);
-            first_half(stage);
-            second_half(stage, [&](int c) { copy_one(stage + 2, c); });
-            copied();
+            if (left == XS) {
+                xnext = 0;
+                if (more) sources_x();
+                else xrecords = 0;
+            }
+            if (left == WS) {
+                wnext = 0;
+                if (more) sources_w();
+                else wrecords = 0;
+            }
+            mask(xnext, xoff);
+            mask(wnext, woff);
+            half_step(xf[0], wf[0], [&](int r) { fetch_one(xslot, wslot, 1, r, xf[1], wf[1]); }, [](int) {});
+            // Everyone has read this step, and the next one has arrived; what the deeper buffer gets, last in a step, has a step
+            // more.  (Behind an item's results everything is awaited: stores are counted too.)
+            if (left < length) arrive<LATE>();
+            else arrive<0>();
+            const int xfree = xslot, wfree = wslot;
+            xslot = xslot == XS - 1 ? 0 : xslot + 1;
+            wslot = wslot == WS - 1 ? 0 : wslot + 1;
+            half_step(xf[1], wf[1], [&](int r) { fetch_one(xslot, wslot, 0, r, xf[0], wf[0]); }, [&](int c) {
+                if constexpr (XS > WS) c < WALL ? copy_w(wfree, c) : copy_x(xfree, c - WALL);
+                else c < XC ? copy_x(xfree, c) : copy_w(wfree, c - XC);
+            });
+            asm volatile("" ::: "memory");
+            on(xbase, xplace);
+            on(wbase, wplace);
         }
 
         const int lane = lane_here();
@@ -527,16 +554,16 @@ constexpr int MOST_PIECES = 8;
 // steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full`; every round
 // has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.  Pieces are added up by a second kernel,
 // which costs `join` and `sum` for every million numbers that it reads.  Fitted to 600 products of 5 to 32768 rows, 16 to 9728
-// outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8 pieces: the plan found by it takes 1.023 times
-// what the best one does in the geometric mean (1.38 times at most, where few outputs meet many rows).
+// outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8 pieces, inputs changing
+// from call to call: the plan found by it takes 1.014 times what the best one does in the geometric mean (1.37 times at most).
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;
 };
 constexpr TileCost COST[TILES] = {
-    {64, 64, 4, 0.252f, 0.890f, 1.78f, 0.44f, 2.73f, 2.23f, 2.17f}, {128, 128, 2, 0.402f, 1.130f, 3.32f, 0.67f, 2.32f, 1.95f, 1.53f},
-    {256, 160, 1, 0.692f, 1.242f, 4.42f, 0.73f, 2.05f, 0.f, 0.f},   {256, 192, 1, 0.752f, 1.374f, 4.94f, 0.81f, 2.14f, 0.f, 0.f},
-    {256, 256, 1, 0.949f, 1.672f, 6.48f, 0.83f, 1.86f, 0.f, 0.f}};
+    {64, 64, 4, 0.357f, 0.930f, 2.05f, 0.64f, 2.46f, 2.22f, 2.27f}, {128, 128, 2, 0.464f, 1.189f, 3.65f, 0.61f, 2.44f, 2.05f, 1.54f},
+    {256, 160, 1, 0.712f, 1.230f, 5.40f, 0.76f, 1.85f, 0.f, 0.f},   {256, 192, 1, 0.791f, 1.351f, 6.05f, 0.79f, 1.54f, 0.f, 0.f},
+    {256, 256, 1, 1.042f, 1.757f, 7.30f, 0.86f, 1.57f, 0.f, 0.f}};
 
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
@@ -557,9 +584,9 @@ Plan plan_for(long long M, int N, int K, int most_pieces)
     Plan best = {T64x64, 1};
     float least = cost_of(COST[T64x64], M, N, K, 1);
     for (int t = 0; t < TILES; ++t) {
-        // (a piece has two steps at least; larger tiles have work enough, or few steps)
+        // (a piece has three steps at least; larger tiles have work enough, or few steps)
         const int most = t <= T128x128 ? most_pieces : 1;
-        for (int pieces = 1; pieces <= most && (pieces == 1 || 2 * pieces * STEP <= K); ++pieces) {
+        for (int pieces = 1; pieces <= most && (pieces == 1 || 3 * pieces * STEP <= K); ++pieces) {
             const float c = cost_of(COST[t], M, N, K, pieces);
             if (c < least) { least = c; best = {(Tile)t, pieces}; }
         }
