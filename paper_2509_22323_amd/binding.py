@@ -168,6 +168,7 @@ class _NoNative:
     def _takes_nothing(self, *args):
         return None
     dense = block_sparse = joint = joint_select = select = store = reuse = _takes_nothing
+    linear = modulate = table = qk_norm_rope = rope = _takes_nothing
 
 
 def _load_native():
@@ -194,7 +195,8 @@ def _load_native():
         return _native
     module.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "rapid_attn_dense", "rapid_attn_block_sparse", "rapid_attn_joint", "rapid_attn_joint_select", "rapid_mask_select",
-        "rapid_cache_store", "rapid_cache_reuse")))
+        "rapid_cache_store", "rapid_cache_reuse", "rapid_linear", "rapid_linear_workspace_bytes", "rapid_norm_modulate",
+        "rapid_rope_table", "rapid_qk_norm_rope", "rapid_rope")))
     _native = module
     return module
 
@@ -617,6 +619,10 @@ def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residu
     contiguous; weight [N,K]; bias [N]; gate [B,N] or [N]; activation "none", "silu" or "gelu_tanh".  residual may be out.
     `workspace`: CUDA uint8 tensor of at least rapid_linear_workspace_bytes(B*n, N, K) bytes; allocated with torch if None.
     Returns out."""
+    status = (_native or _load_native()).linear(x, weight, out, bias, activation, gate, residual, workspace)
+    if status is not None:
+        _check(status)
+        return out
     import torch
     xr, B, n, K = _rows("x", x)
     device = x.get_device()
@@ -654,6 +660,10 @@ def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residu
 def rapid_norm_modulate(x, out, scale=None, shift=None, eps=1e-6):
     """out <- (x - mean) / sqrt(variance + eps) * (1 + scale) + shift over the last dimension.  x, out [B,n,C] (or [n,C]): CUDA
     bf16, last dimension contiguous; scale, shift [B,C] or [C], both or neither.  out may be x.  Returns out."""
+    status = (_native or _load_native()).modulate(x, out, scale, shift, eps)
+    if status is not None:
+        _check(status)
+        return out
     xr, B, n, C = _rows("x", x)
     device = x.get_device()
     outr, *shape = _rows("out", out, device)
@@ -672,6 +682,10 @@ def rapid_rope_table(positions, axes, table, magnitude=1.0):
     """table[..., i, :] <- magnitude * (cos, sin) of the angle of pair i at each position.  positions: CUDA int32
     [..., len(axes)] contiguous; axes: sequence of RopeAxis; table: CUDA float32 [..., rot / 2, 2] contiguous, rot the sum of
     the axes' dims.  Returns table."""
+    status = (_native or _load_native()).table(positions, axes, table, magnitude)
+    if status is not None:
+        _check(status)
+        return table
     import torch
     if not (isinstance(positions, torch.Tensor) and positions.is_cuda and positions.dtype == torch.int32
             and positions.dim() >= 2 and positions.is_contiguous()):
@@ -750,6 +764,10 @@ def rapid_qk_norm_rope(segments, weights=None, table=None, layout="interleaved",
     q_out and k_out theirs; q_out may be q and k_out k.  weights: a (q_weight, k_weight) for each segment, [D] or None;
     table: float32 [N, rot/2, 2] (rapid_rope_table) over the joint tokens, or [B, N, rot/2, 2], or None: the norm alone;
     layout "interleaved" or "half".  Returns the outputs, (q_out, k_out) of one segment after the other."""
+    status = (_native or _load_native()).qk_norm_rope(segments, weights, table, layout, eps)
+    if status is not None:
+        _check(status)
+        return [t for seg in segments for t in seg[2:]]
     descr, B, H, D, table_ptr, table_stride, rot, lay, device = _qk_rows(segments, weights, table, layout)
     _check(_on_device(device, lambda stream: library().rapid_qk_norm_rope(
         descr, len(segments), B, H, D, float(eps), table_ptr, table_stride, rot, lay, stream)))
@@ -758,6 +776,10 @@ def rapid_qk_norm_rope(segments, weights=None, table=None, layout="interleaved",
 
 def rapid_rope(segments, table, layout="interleaved"):
     """The rotation of rapid_qk_norm_rope alone.  Returns the outputs."""
+    status = (_native or _load_native()).rope(segments, None, table, layout)
+    if status is not None:
+        _check(status)
+        return [t for seg in segments for t in seg[2:]]
     descr, B, H, D, table_ptr, table_stride, rot, lay, device = _qk_rows(segments, None, table, layout)
     _check(_on_device(device, lambda stream: library().rapid_rope(
         descr, len(segments), B, H, D, table_ptr, table_stride, rot, lay, stream)))

@@ -8,11 +8,14 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <limits.h>
+#include <string.h>
 
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "rapid_attn.h"
 #include "rapid_cache.h"
+#include "rapid_layer.h"
 #include "rapid_mask.h"
 
 namespace {
@@ -26,6 +29,12 @@ decltype(&rapid_attn_joint_select) attn_joint_select;
 decltype(&rapid_mask_select) mask_select;
 decltype(&rapid_cache_store) cache_store;
 decltype(&rapid_cache_reuse) cache_reuse;
+decltype(&rapid_linear) layer_linear;
+decltype(&rapid_linear_workspace_bytes) layer_linear_bytes;
+decltype(&rapid_norm_modulate) layer_modulate;
+decltype(&rapid_rope_table) layer_table;
+decltype(&rapid_qk_norm_rope) layer_qk;
+decltype(&rapid_rope) layer_rope;
 
 // A tensor of exactly that class with memory of its own on a GPU; else null.
 const at::Tensor* plain(PyObject* o)
@@ -293,11 +302,210 @@ PyObject* residual(PyObject* const* a, Py_ssize_t n, Call call)
 PyObject* store(PyObject*, PyObject* const* a, Py_ssize_t n) { return residual(a, n, cache_store); }
 PyObject* reuse(PyObject*, PyObject* const* a, Py_ssize_t n) { return residual(a, n, cache_reuse); }
 
+// ---- a layer around its attention: tensors of the current device alone (the Python form makes another one current)
+bool current(int device) { return c10::impl::getDeviceGuardImpl(at::kCUDA)->getDevice().index() == device; }
+
+// [B, n, width] or [n, width] with a contiguous last dimension
+struct Rows3 {
+    rapid_rows rows;
+    int B, n, width, device;
+};
+bool rows3(PyObject* o, Rows3& x)
+{
+    const at::Tensor* t = of(o, at::kBFloat16);
+    if (!t || (t->dim() != 2 && t->dim() != 3)) return false;
+    const int d = (int)t->dim();
+    x.B = 1;
+    if ((d == 3 && !size(t->size(0), x.B)) || !size(t->size(d - 2), x.n) || !size(t->size(d - 1), x.width)) return false;
+    if (t->stride(d - 1) != 1 && x.width != 1) return false;
+    x.rows = {t->data_ptr(), d == 3 ? t->stride(0) : 0, t->stride(d - 2)};
+    x.device = t->get_device();
+    return true;
+}
+// None, or [B, width] or [width] with a contiguous last dimension
+bool vectors(PyObject* o, const Rows3& like, const void*& p, long long& stride)
+{
+    p = nullptr;
+    stride = 0;
+    if (o == Py_None) return true;
+    const at::Tensor* t = of(o, at::kBFloat16);
+    if (!t || (t->dim() != 1 && t->dim() != 2) || t->get_device() != like.device) return false;
+    const int d = (int)t->dim();
+    if (t->size(d - 1) != like.width || (t->stride(d - 1) != 1 && like.width != 1)) return false;
+    if (d == 2) {
+        if (t->size(0) != like.B) return false;
+        stride = t->stride(0);
+    }
+    p = t->data_ptr();
+    return true;
+}
+bool is(PyObject* o, const char* text) { return PyUnicode_CheckExact(o) && PyUnicode_CompareWithASCIIString(o, text) == 0; }
+
+// (x, weight, out, bias, activation, gate, residual, workspace or None where none is made use of)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows3 x, out, res;
+    if (n != 8 || !rows3(a[0], x) || !rows3(a[2], out) || out.B != x.B || out.n != x.n || out.device != x.device || !current(x.device)) Py_RETURN_NONE;
+    const at::Tensor* w = of(a[1], at::kBFloat16);
+    if (!w || w->dim() != 2 || w->size(0) != out.width || w->size(1) != x.width || w->get_device() != x.device) Py_RETURN_NONE;
+    if (w->stride(1) != 1 && x.width != 1) Py_RETURN_NONE;
+    const void *bias, *gate;
+    long long unused, gate_stride;
+    if (!vectors(a[3], out, bias, unused) || (bias && THPVariable_Unpack(a[3]).dim() != 1) || !vectors(a[5], out, gate, gate_stride)) Py_RETURN_NONE;
+    const int activation = is(a[4], "none") ? RAPID_ACT_NONE : is(a[4], "silu") ? RAPID_ACT_SILU : is(a[4], "gelu_tanh") ? RAPID_ACT_GELU_TANH : -1;
+    if (activation < 0) Py_RETURN_NONE;
+    if (a[6] != Py_None && (!rows3(a[6], res) || res.B != out.B || res.n != out.n || res.width != out.width || res.device != x.device)) Py_RETURN_NONE;
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (a[7] != Py_None) {
+        const at::Tensor* t = plain(a[7]);
+        if (!t || !t->is_contiguous() || t->get_device() != x.device) Py_RETURN_NONE;
+        ws = t->data_ptr();
+        bytes = t->nbytes();
+    } else if (layer_linear_bytes((long long)x.B * x.n, out.width, x.width) != 0) Py_RETURN_NONE;
+    const void* weight = w->data_ptr();
+    const long long w_stride = out.width > 1 ? w->stride(0) : x.width;
+    const rapid_rows* residual = a[6] != Py_None ? &res.rows : nullptr;
+    return launch(x.device, [&](void* s) {
+        return layer_linear(&x.rows, weight, w_stride, bias, &out.rows, activation, gate, gate_stride, residual, x.B, x.n, out.width, x.width,
+                            ws, bytes, s);
+    });
+}
+
+// (x, out, scale, shift, eps)
+PyObject* modulate(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows3 x, out;
+    float eps;
+    const void *scale, *shift;
+    long long scale_stride, shift_stride;
+    if (n != 5 || !rows3(a[0], x) || !rows3(a[1], out) || out.B != x.B || out.n != x.n || out.width != x.width || out.device != x.device) Py_RETURN_NONE;
+    if (!current(x.device) || !vectors(a[2], x, scale, scale_stride) || !vectors(a[3], x, shift, shift_stride) || !scale != !shift) Py_RETURN_NONE;
+    if (!number(a[4], eps)) Py_RETURN_NONE;
+    return launch(x.device, [&](void* s) {
+        return layer_modulate(&x.rows, &out.rows, scale, scale_stride, shift, shift_stride, x.B, x.n, x.width, eps, s);
+    });
+}
+
+// (positions, axes: a list or tuple of rapid_rope_axis, table, magnitude)
+PyObject* table(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 4 || (!PyList_CheckExact(a[1]) && !PyTuple_CheckExact(a[1]))) Py_RETURN_NONE;
+    const at::Tensor *p = of(a[0], at::kInt), *t = of(a[2], at::kFloat);
+    const Py_ssize_t axes = PySequence_Fast_GET_SIZE(a[1]);
+    float magnitude;
+    if (!p || !t || axes < 1 || axes > 8 || !p->is_contiguous() || !t->is_contiguous() || t->get_device() != p->get_device()) Py_RETURN_NONE;
+    if (!current(p->get_device()) || p->dim() < 2 || t->dim() != p->dim() + 1 || p->size(-1) != axes || t->size(-1) != 2) Py_RETURN_NONE;
+    if (p->sizes().slice(0, p->dim() - 1) != t->sizes().slice(0, t->dim() - 2) || !number(a[3], magnitude)) Py_RETURN_NONE;
+    rapid_rope_axis axis[8];
+    int64_t dims = 0;
+    for (Py_ssize_t i = 0; i < axes; ++i) {
+        Py_buffer b;
+        PyObject* o = PySequence_Fast_GET_ITEM(a[1], i);
+        if (!PyObject_CheckBuffer(o)) Py_RETURN_NONE;
+        if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) { PyErr_Clear(); Py_RETURN_NONE; }
+        const bool fits = b.len == (Py_ssize_t)sizeof(rapid_rope_axis);
+        if (fits) memcpy(&axis[i], b.buf, sizeof(rapid_rope_axis));
+        PyBuffer_Release(&b);
+        if (!fits) Py_RETURN_NONE;
+        dims += axis[i].dim;
+    }
+    if (dims != 2 * t->size(-2)) Py_RETURN_NONE;
+    const int* positions = (const int*)p->data_ptr();
+    float* out = (float*)t->data_ptr();
+    const long long tokens = p->numel() / axes;
+    const double scale = PyFloat_CheckExact(a[3]) ? PyFloat_AS_DOUBLE(a[3]) : (double)magnitude;
+    return launch(p->get_device(), [&](void* s) { return layer_table(positions, tokens, (int)axes, axis, scale, out, s); });
+}
+
+// (segments of (q, k, q_out, k_out), weights or None, table or None, layout): both forms
+struct QkCall {
+    rapid_qk_segment seg[2];
+    int n, B, H, D, device, rot, layout;
+    const float* table;
+    long long table_stride;
+};
+bool qk_call(PyObject* const* a, QkCall& x)
+{
+    if (!PyList_CheckExact(a[0]) && !PyTuple_CheckExact(a[0])) return false;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[0]);
+    const bool weighted = a[1] != Py_None;
+    if (n != 1 && n != 2) return false;
+    if (weighted && ((!PyList_CheckExact(a[1]) && !PyTuple_CheckExact(a[1])) || PySequence_Fast_GET_SIZE(a[1]) != n)) return false;
+    int64_t tokens = 0;
+    x.n = (int)n;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* one = PySequence_Fast_GET_ITEM(a[0], i);
+        if ((!PyList_CheckExact(one) && !PyTuple_CheckExact(one)) || PySequence_Fast_GET_SIZE(one) != 4) return false;
+        const at::Tensor* t[4];
+        for (int j = 0; j < 4; ++j) {
+            t[j] = of(PySequence_Fast_GET_ITEM(one, j), at::kBFloat16);
+            if (!t[j] || t[j]->dim() != 4 || t[j]->stride(3) != 1) return false;
+            if (j > 0 && (t[j]->sizes() != t[0]->sizes() || t[j]->get_device() != t[0]->get_device())) return false;
+        }
+        if (t[1]->strides() != t[0]->strides() || t[3]->strides() != t[2]->strides()) return false;
+        int B, H, D;
+        rapid_qk_segment& g = x.seg[i];
+        g = {};
+        if (!size(t[0]->size(0), B) || !size(t[0]->size(1), H) || !size(t[0]->size(2), g.n) || !size(t[0]->size(3), D)) return false;
+        if (i == 0) { x.B = B; x.H = H; x.D = D; x.device = t[0]->get_device(); }
+        else if (B != x.B || H != x.H || D != x.D || t[0]->get_device() != x.device) return false;
+        g.q = t[0]->data_ptr(); g.k = t[1]->data_ptr(); g.q_out = t[2]->data_ptr(); g.k_out = t[3]->data_ptr();
+        g.in_stride_b = t[0]->stride(0); g.in_stride_h = t[0]->stride(1); g.in_stride_n = t[0]->stride(2);
+        g.out_stride_b = t[2]->stride(0); g.out_stride_h = t[2]->stride(1); g.out_stride_n = t[2]->stride(2);
+        if (weighted) {
+            PyObject* two = PySequence_Fast_GET_ITEM(a[1], i);
+            if ((!PyList_CheckExact(two) && !PyTuple_CheckExact(two)) || PySequence_Fast_GET_SIZE(two) != 2) return false;
+            const void** to[2] = {&g.q_weight, &g.k_weight};
+            for (int j = 0; j < 2; ++j) {
+                PyObject* w = PySequence_Fast_GET_ITEM(two, j);
+                if (w == Py_None) continue;
+                const at::Tensor* v = packed(w, at::kBFloat16, x.device);
+                if (!v || v->dim() != 1 || v->size(0) != D) return false;
+                *to[j] = v->data_ptr();
+            }
+        }
+        tokens += g.n;
+    }
+    x.layout = is(a[3], "interleaved") ? RAPID_ROPE_INTERLEAVED : is(a[3], "half") ? RAPID_ROPE_HALVES : -1;
+    x.table = nullptr;
+    x.table_stride = 0;
+    x.rot = 0;
+    if (x.layout < 0 || !current(x.device)) return false;
+    if (a[2] == Py_None) return true;
+    const at::Tensor* t = packed(a[2], at::kFloat, x.device);
+    if (!t || (t->dim() != 3 && t->dim() != 4) || t->size(-1) != 2 || t->size(-3) != tokens || t->size(-2) > 64) return false;
+    if (t->dim() == 4) {
+        if (t->size(0) != x.B) return false;
+        x.table_stride = t->stride(0);
+    }
+    x.rot = 2 * (int)t->size(-2);
+    x.table = (const float*)t->data_ptr();
+    return true;
+}
+
+// (segments, weights, table, layout, eps)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    QkCall x;
+    float eps;
+    if (n != 5 || !qk_call(a, x) || !number(a[4], eps)) Py_RETURN_NONE;
+    return launch(x.device, [&](void* s) { return layer_qk(x.seg, x.n, x.B, x.H, x.D, eps, x.table, x.table_stride, x.rot, x.layout, s); });
+}
+
+// (segments, None, table, layout)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    QkCall x;
+    if (n != 4 || a[1] != Py_None || a[2] == Py_None || !qk_call(a, x)) Py_RETURN_NONE;
+    return launch(x.device, [&](void* s) { return layer_rope(x.seg, x.n, x.B, x.H, x.D, x.table, x.table_stride, x.rot, x.layout, s); });
+}
+
 // bind(address of each entry point, ..): of the library that binding.py has loaded
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long p[7];
-    if (!PyArg_ParseTuple(args, "KKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6])) return nullptr;
+    unsigned long long p[13];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12])) return nullptr;
     attn_dense = (decltype(attn_dense))p[0];
     attn_block_sparse = (decltype(attn_block_sparse))p[1];
     attn_joint = (decltype(attn_joint))p[2];
@@ -305,6 +513,12 @@ PyObject* bind(PyObject*, PyObject* args)
     mask_select = (decltype(mask_select))p[4];
     cache_store = (decltype(cache_store))p[5];
     cache_reuse = (decltype(cache_reuse))p[6];
+    layer_linear = (decltype(layer_linear))p[7];
+    layer_linear_bytes = (decltype(layer_linear_bytes))p[8];
+    layer_modulate = (decltype(layer_modulate))p[9];
+    layer_table = (decltype(layer_table))p[10];
+    layer_qk = (decltype(layer_qk))p[11];
+    layer_rope = (decltype(layer_rope))p[12];
     PyObject* c = PyImport_ImportModule("torch._C");
     if (!c) return nullptr;
     Py_XSETREF(current_stream, PyObject_GetAttrString(c, "_cuda_getCurrentRawStream"));
@@ -326,7 +540,8 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 }
 #define NATIVE(f) {#f, (PyCFunction)(void (*)(void))guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, NATIVE(dense), NATIVE(block_sparse), NATIVE(select), NATIVE(joint),
-                         NATIVE(joint_select), NATIVE(store), NATIVE(reuse), {nullptr, nullptr, 0, nullptr}};
+                         NATIVE(joint_select), NATIVE(store), NATIVE(reuse), NATIVE(linear), NATIVE(modulate), NATIVE(table),
+                         NATIVE(qk_norm_rope), NATIVE(rope), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "native_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

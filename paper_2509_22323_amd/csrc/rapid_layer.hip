@@ -263,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void qk_rows_kernel(QkParams p)
 // ---------------------------------------------------------------------------
 // The table
 // ---------------------------------------------------------------------------
-constexpr int MAX_PAIRS = 64;
+constexpr int MAX_PAIRS = 64, TABLE_GROUPS = 4096;
 struct TableParams {
     const int* positions;
     float* table;
@@ -274,16 +274,31 @@ struct TableParams {
     unsigned char axis[MAX_PAIRS];
 };
 
+// magnitude * (cos, sin) of a number of turns, in fp64 as far as fp32 can tell: taken to the nearest quarter, where Taylor's sums of
+// six terms are off by 1.1e-10 (cosine) and 7e-12 (sine) at most.  (The library's fp64 sincospi instead: 31 -> 44 us for 264 K tokens of 64 pairs.)
+__device__ __forceinline__ float2 turned(double turns, double magnitude)
+{
+    const double part = turns - rint(turns), quarters = rint(4.0 * part);
+    const double a = (part - 0.25 * quarters) * (2.0 * M_PI), q = a * a;
+    const double s = a * fma(q, fma(q, fma(q, fma(q, fma(q, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);
+    const double c = fma(q, fma(q, fma(q, fma(q, fma(q, -1.0 / 3628800, 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
+    const int k = (int)quarters & 3;                       // cos, sin = (c, s), (-s, c), (-c, -s), (s, -c)
+    const double x = k & 1 ? s : c, y = k & 1 ? c : s;
+    return make_float2((float)(k == 1 || k == 2 ? -magnitude * x : magnitude * x), (float)(k >= 2 ? -magnitude * y : magnitude * y));
+}
+
+// A lane stays with two neighbouring pairs and goes over tokens; 16 bytes a store.
 __global__ __launch_bounds__(THREADS) void rope_table_kernel(TableParams p)
 {
-    const long long at = (long long)blockIdx.x * THREADS + threadIdx.x;
-    if (at >= p.tokens * p.pairs) return;
-    const long long t = at / p.pairs;
-    const int i = (int)(at - t * p.pairs);
-    const double angle = p.positions[t * p.axes + p.axis[i]] * p.turns[i];
-    double s, c;
-    sincospi(2.0 * (angle - rint(angle)), &s, &c);
-    *(float2*)(p.table + 2 * at) = make_float2((float)(p.magnitude * c), (float)(p.magnitude * s));
+    const int lanes = p.pairs / 2, tokens = THREADS / lanes, own = threadIdx.x / lanes, i = 2 * (threadIdx.x - own * lanes);
+    if (own >= tokens) return;
+    const double f0 = p.turns[i], f1 = p.turns[i + 1];
+    const int a0 = p.axis[i], a1 = p.axis[i + 1];
+    for (long long t = (long long)blockIdx.x * tokens + own; t < p.tokens; t += (long long)gridDim.x * tokens) {
+        const int* at = p.positions + t * p.axes;
+        const float2 one = turned(at[a0] * f0, p.magnitude), two = turned(at[a1] * f1, p.magnitude);
+        *(f32x4*)(p.table + 2 * (t * p.pairs + i)) = f32x4{one.x, one.y, two.x, two.y};
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -460,9 +475,8 @@ int rapid_rope_table(const int* positions, long long tokens, int n_axes, const r
     p.tokens = tokens;
     p.magnitude = magnitude;
     p.axes = n_axes;
-    const long long blocks = (tokens * p.pairs + THREADS - 1) / THREADS;
-    if (blocks * THREADS >= (1LL << 32)) return RAPID_ERR_SHAPE;
-    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, (hipStream_t)stream, p);
+    const long long each = THREADS / (p.pairs / 2), blocks = (tokens + each - 1) / each;
+    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)(blocks < TABLE_GROUPS ? blocks : TABLE_GROUPS)), dim3(THREADS), 0, (hipStream_t)stream, p);
     return launched();
 }
 
