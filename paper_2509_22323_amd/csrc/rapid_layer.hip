@@ -160,7 +160,10 @@ struct QkParams {
     bool heads_first;                  // neighbouring lane groups take neighbouring heads (else tokens)
 };
 
-constexpr int HEADS = 4;               // heads of a lane group: 8 rows (queries and keys) in flight
+// Heads of a lane group: 4 rows (queries and keys) in flight.  One head: 34 us at 4608 tokens of 24 heads of 128, two 29.5, four
+// 30.5 (fewer workgroups, the last of them alone); small calls are faster the more workgroups there are.  Loads past the caches
+// would gain 6 % where the rows come from memory and cost 20 % where the projection has just left them in the caches.
+constexpr int HEADS = 2;
 
 // A group of D / 8 lanes takes one token: its row of the table, and heads part, part + parts, .. of queries and keys.
 template <int D, bool NORM, int LAYOUT>            // LAYOUT -1: no rotation
@@ -233,7 +236,7 @@ __global__ __launch_bounds__(THREADS) void qk_rows_kernel(QkParams p)
                 float square = 0.f;
 #pragma unroll
                 for (int q = 0; q < 8; ++q) square = __builtin_fmaf(e.v[q], e.v[q], square);
-                const float inv = 1.0f / sqrtf(sum_over<LANES>(square) * (1.0f / D) + p.eps);
+                const float inv = __builtin_amdgcn_rsqf(__builtin_fmaf(sum_over<LANES>(square), 1.0f / D, p.eps));
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                     e.v[q] *= inv * w.v[q];
@@ -275,19 +278,23 @@ struct TableParams {
 };
 
 // magnitude * (cos, sin) of a number of turns, in fp64 as far as fp32 can tell: taken to the nearest quarter, where Taylor's sums of
-// six terms are off by 1.1e-10 (cosine) and 7e-12 (sine) at most.  (The library's fp64 sincospi instead: 31 -> 44 us for 264 K tokens of 64 pairs.)
+// six and five terms are off by 1.1e-10 (cosine) and 1.8e-9 (sine) at most, 0.03 of half a step of fp32.  (With the library's
+// fp64 sincospi 264 K tokens of 64 pairs take 62 us, stores of 8 bytes and a 64-bit division a pair included.)
 __device__ __forceinline__ float2 turned(double turns, double magnitude)
 {
-    const double part = turns - rint(turns), quarters = rint(4.0 * part);
-    const double a = (part - 0.25 * quarters) * (2.0 * M_PI), q = a * a;
-    const double s = a * fma(q, fma(q, fma(q, fma(q, fma(q, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);
-    const double c = fma(q, fma(q, fma(q, fma(q, fma(q, -1.0 / 3628800, 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
-    const int k = (int)quarters & 3;                       // cos, sin = (c, s), (-s, c), (-c, -s), (s, -c)
-    const double x = k & 1 ? s : c, y = k & 1 ? c : s;
-    return make_float2((float)(k == 1 || k == 2 ? -magnitude * x : magnitude * x), (float)(k >= 2 ? -magnitude * y : magnitude * y));
+    constexpr double WHOLE = 6755399441055744.0;            // 1.5 * 2^52: a sum with it is rounded to a whole number, in its low bits
+    const double shifted = fma(4.0, turns, WHOLE);
+    const double a = fma(-0.25, shifted - WHOLE, turns) * (2.0 * M_PI), q = a * a;
+    double s = a * fma(q, fma(q, fma(q, fma(q, 1.0 / 362880, -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);
+    double c = fma(q, fma(q, fma(q, fma(q, fma(q, -1.0 / 3628800, 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
+    if (magnitude != 1.0) { s *= magnitude; c *= magnitude; }
+    const unsigned k = (unsigned)__double2loint(shifted);   // quarters: cos, sin = (c, s), (-s, c), (-c, -s), (s, -c)
+    const float fs = (float)s, fc = (float)c, x = k & 1u ? fs : fc, y = k & 1u ? fc : fs;
+    return make_float2(__uint_as_float(__float_as_uint(x) ^ ((k + 1u & 2u) << 30)), __uint_as_float(__float_as_uint(y) ^ ((k & 2u) << 30)));
 }
 
-// A lane stays with two neighbouring pairs and goes over tokens; 16 bytes a store.
+// A lane stays with two neighbouring pairs and goes over tokens; 16 bytes a store, past the caches (264 K tokens of 64 pairs, 138 MB:
+// 38 -> 25 us; 17 K tokens 5.4 -> 5.1).
 __global__ __launch_bounds__(THREADS) void rope_table_kernel(TableParams p)
 {
     const int lanes = p.pairs / 2, tokens = THREADS / lanes, own = threadIdx.x / lanes, i = 2 * (threadIdx.x - own * lanes);
@@ -297,7 +304,7 @@ __global__ __launch_bounds__(THREADS) void rope_table_kernel(TableParams p)
     for (long long t = (long long)blockIdx.x * tokens + own; t < p.tokens; t += (long long)gridDim.x * tokens) {
         const int* at = p.positions + t * p.axes;
         const float2 one = turned(at[a0] * f0, p.magnitude), two = turned(at[a1] * f1, p.magnitude);
-        *(f32x4*)(p.table + 2 * (t * p.pairs + i)) = f32x4{one.x, one.y, two.x, two.y};
+        __builtin_nontemporal_store(f32x4{one.x, one.y, two.x, two.y}, (f32x4*)(p.table + 2 * (t * p.pairs + i)));
     }
 }
 
