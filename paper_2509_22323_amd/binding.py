@@ -575,6 +575,23 @@ def rapid_attn_joint_select(segments, block=128, kv_len=None, kv_lens=None, text
 
 
 # ---------------------------------------------------------------- a layer around its attention
+_LAYER_ERRORS = {
+    -1: "a required pointer is NULL",
+    -2: "invalid shape: a size or stride out of range, or rows of an output that share elements",
+    -3: "unsupported: widths of inputs and rows are multiples of 8 (a norm's 16384 at most), heads 64 or 128 wide, the rotated "
+        "part a multiple of 16 and no more than the head; see include/rapid_layer.h",
+    -4: "a pointer or stride is not aligned (16 bytes, 8 elements; outputs, biases and gates of rapid_linear 2 bytes)",
+    -5: "the workspace is too small or not aligned to 16 bytes",
+    -6: "the HIP runtime refused a launch",
+    -7: "an output begins where an input or another output does",
+}
+
+
+def _check_layer(status: int):
+    if status != 0:
+        raise RapidAttnError(status, _LAYER_ERRORS.get(status, "unknown status"))
+
+
 def _on_device(device, call):
     """call(stream) with torch's current stream of `device`, which is made the current device meanwhile (the default stream's
     handle names none)."""
@@ -621,7 +638,7 @@ def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residu
     Returns out."""
     status = (_native or _load_native()).linear(x, weight, out, bias, activation, gate, residual, workspace)
     if status is not None:
-        _check(status)
+        _check_layer(status)
         return out
     import torch
     xr, B, n, K = _rows("x", x)
@@ -651,7 +668,7 @@ def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residu
               and workspace.get_device() == device):
         raise TypeError("workspace must be a contiguous CUDA tensor on x's device")
     ws_ptr, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check(_on_device(device, lambda stream: library().rapid_linear(
+    _check_layer(_on_device(device, lambda stream: library().rapid_linear(
         xr, weight.data_ptr(), weight.stride(0) if N > 1 else K, bias_ptr, outr, ACTIVATIONS[activation], gate_ptr, gate_stride, res,
         B, n, N, K, ws_ptr, ws_bytes, stream)))
     return out
@@ -662,7 +679,7 @@ def rapid_norm_modulate(x, out, scale=None, shift=None, eps=1e-6):
     bf16, last dimension contiguous; scale, shift [B,C] or [C], both or neither.  out may be x.  Returns out."""
     status = (_native or _load_native()).modulate(x, out, scale, shift, eps)
     if status is not None:
-        _check(status)
+        _check_layer(status)
         return out
     xr, B, n, C = _rows("x", x)
     device = x.get_device()
@@ -673,7 +690,7 @@ def rapid_norm_modulate(x, out, scale=None, shift=None, eps=1e-6):
         raise ValueError("scale and shift: both or neither")
     scale_ptr, scale_stride = _vectors("scale", scale, B, C, device)
     shift_ptr, shift_stride = _vectors("shift", shift, B, C, device)
-    _check(_on_device(device, lambda stream: library().rapid_norm_modulate(
+    _check_layer(_on_device(device, lambda stream: library().rapid_norm_modulate(
         xr, outr, scale_ptr, scale_stride, shift_ptr, shift_stride, B, n, C, float(eps), stream)))
     return out
 
@@ -684,7 +701,7 @@ def rapid_rope_table(positions, axes, table, magnitude=1.0):
     the axes' dims.  Returns table."""
     status = (_native or _load_native()).table(positions, axes, table, magnitude)
     if status is not None:
-        _check(status)
+        _check_layer(status)
         return table
     import torch
     if not (isinstance(positions, torch.Tensor) and positions.is_cuda and positions.dtype == torch.int32
@@ -702,7 +719,7 @@ def rapid_rope_table(positions, axes, table, magnitude=1.0):
         raise ValueError(f"positions {tuple(positions.shape)} and table {tuple(table.shape)} do not go with {len(axes)} axes of "
                          f"{pairs} pairs")
     tokens = positions.numel() // len(axes) if axes else 0
-    _check(_on_device(device, lambda stream: library().rapid_rope_table(
+    _check_layer(_on_device(device, lambda stream: library().rapid_rope_table(
         positions.data_ptr(), tokens, len(axes), (RopeAxis * max(len(axes), 1))(*axes), float(magnitude), table.data_ptr(), stream)))
     return table
 
@@ -766,10 +783,10 @@ def rapid_qk_norm_rope(segments, weights=None, table=None, layout="interleaved",
     layout "interleaved" or "half".  Returns the outputs, (q_out, k_out) of one segment after the other."""
     status = (_native or _load_native()).qk_norm_rope(segments, weights, table, layout, eps)
     if status is not None:
-        _check(status)
+        _check_layer(status)
         return [t for seg in segments for t in seg[2:]]
     descr, B, H, D, table_ptr, table_stride, rot, lay, device = _qk_rows(segments, weights, table, layout)
-    _check(_on_device(device, lambda stream: library().rapid_qk_norm_rope(
+    _check_layer(_on_device(device, lambda stream: library().rapid_qk_norm_rope(
         descr, len(segments), B, H, D, float(eps), table_ptr, table_stride, rot, lay, stream)))
     return [t for seg in segments for t in seg[2:]]
 
@@ -778,9 +795,9 @@ def rapid_rope(segments, table, layout="interleaved"):
     """The rotation of rapid_qk_norm_rope alone.  Returns the outputs."""
     status = (_native or _load_native()).rope(segments, None, table, layout)
     if status is not None:
-        _check(status)
+        _check_layer(status)
         return [t for seg in segments for t in seg[2:]]
     descr, B, H, D, table_ptr, table_stride, rot, lay, device = _qk_rows(segments, None, table, layout)
-    _check(_on_device(device, lambda stream: library().rapid_rope(
+    _check_layer(_on_device(device, lambda stream: library().rapid_rope(
         descr, len(segments), B, H, D, table_ptr, table_stride, rot, lay, stream)))
     return [t for seg in segments for t in seg[2:]]
