@@ -100,7 +100,7 @@ typedef enum {
 typedef struct rapid_rope_axis {
     int dim;                                  /* even, >= 2 (RAPID_ROPE_NTK: >= 4)                     */
     int scaling;                              /* a rapid_rope_scaling                                  */
-    double theta;                             /* > 0                                                   */
+    double theta;                             /* > 0, no frequency of 65536 turns a position or more   */
     double factor;                            /* > 0; not looked at by RAPID_ROPE_PLAIN                */
     double original_length;                   /* > 0          }                                        */
     double beta_fast, beta_slow;              /* fast > slow  } looked at by RAPID_ROPE_BY_PARTS alone */

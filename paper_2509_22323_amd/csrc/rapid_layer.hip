@@ -471,7 +471,7 @@ int rapid_rope_table(const int* positions, long long tokens, int n_axes, const r
                 f *= g + (1.0 - g) / x.factor;
             }
             p.turns[p.pairs] = f / (2.0 * M_PI);
-            if (!isfinite(p.turns[p.pairs])) return RAPID_ERR_UNSUPPORTED;
+            if (!(p.turns[p.pairs] < 65536.0)) return RAPID_ERR_UNSUPPORTED;       // (reduction takes 2^50 turns)
             p.axis[p.pairs++] = (unsigned char)a;
         }
     }

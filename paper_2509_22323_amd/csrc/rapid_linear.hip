@@ -62,8 +62,9 @@ __device__ __forceinline__ float activated(float z, int activation)
 {
     if (activation == RAPID_ACT_NONE) return z;
     // z / (1 + exp(-t)): t = z, or, with 1 + tanh(u) = 2 / (1 + exp(-2u)), t = 2u.  exp overflows to inf and the quotient to -0.
-    const float t = activation == RAPID_ACT_SILU ? z : 1.5957691216057308f * z * __builtin_fmaf(0.044715f * z, z, 1.0f);
-    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * t));
+    constexpr float C = 1.5957691216057308f * LOG2E;
+    const float e = activation == RAPID_ACT_SILU ? -LOG2E * z : z * __builtin_fmaf(z * z, -0.044715f * C, -C);
+    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(e));
 }
 
 // What the epilogue adds and multiplies, and writes, eight outputs at a time: rows of odd widths start anywhere, so these accesses
@@ -117,6 +118,7 @@ __device__ __forceinline__ bf16x8 finished(const LinearParams& p, float (&z)[8],
 constexpr int STEP = 64;                               // inputs per step: 128 bytes of a row
 constexpr int ROW = STEP * 2;
 constexpr int CUS = 256;
+constexpr int MOST_PIECES = 8;                         // along K
 constexpr unsigned NOWHERE = 0xC0000000u;              // an offset outside any buffer below
 constexpr unsigned BUFFER = 0x80000100u;               // bytes that a tile's rows may span
 
@@ -437,11 +439,18 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i] = (float)bias[i];
     const float* from = p.partial + (long long)m * p.pitch + n;
-    for (int s = 0; s < p.pieces; ++s, from += (long long)p.M * p.pitch) {
-        const f32x4 a = *(const f32x4*)from, c = *(const f32x4*)(from + 4);
+    f32x4 part[MOST_PIECES][2];                        // all of them on their way before the first is added
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { z[i] += a[i]; z[4 + i] += c[i]; }
-    }
+    for (int s = 0; s < MOST_PIECES; ++s)
+        if (s < p.pieces) {
+            part[s][0] = *(const f32x4*)(from + s * (long long)p.M * p.pitch);
+            part[s][1] = *(const f32x4*)(from + s * (long long)p.M * p.pitch + 4);
+        }
+#pragma unroll
+    for (int s = 0; s < MOST_PIECES; ++s)
+        if (s < p.pieces)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] += part[s][i / 4][i % 4];
     store_eight(p.y + b * p.y_sb + (long long)r * p.y_sn, n, p.N, finished(p, z, gate, residual));
 }
 
@@ -548,7 +557,6 @@ struct Plan {
     Tile tile;
     int pieces;
 };
-constexpr int MOST_PIECES = 8;
 
 // What a product takes, in us.  Its items (tiles times pieces) go to 256 CUs with each slots of them at a time: full rounds, whose
 // steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full`; every round
@@ -584,8 +592,8 @@ Plan plan_for(long long M, int N, int K, int most_pieces)
     Plan best = {T64x64, 1};
     float least = cost_of(COST[T64x64], M, N, K, 1);
     for (int t = 0; t < TILES; ++t) {
-        // (a piece has three steps at least; larger tiles have work enough, or few steps)
-        const int most = t <= T128x128 ? most_pieces : 1;
+        // (a piece has three steps at least; larger tiles have work enough, or few steps; a lane number of the join has 32 bits)
+        const int most = t <= T128x128 && M * N < (1LL << 31) ? most_pieces : 1;
         for (int pieces = 1; pieces <= most && (pieces == 1 || 3 * pieces * STEP <= K); ++pieces) {
             const float c = cost_of(COST[t], M, N, K, pieces);
             if (c < least) { least = c; best = {(Tile)t, pieces}; }

@@ -252,3 +252,98 @@ def test_captured_calls_repeat_what_eager_calls_do():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (table, h, qkv, y)))
+
+
+# ------------------------------------------------------------------------------------- large tensors, both forms of the binding
+def test_offsets_beyond_32_bits():
+    n, C = 1500000, 1536                                                           # 4.6 GB
+    x = torch.zeros((1, n, C), dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 699050, 699051, 1398101, n - 1], device="cuda")
+    x[0, rows] = normal((5, C), 71)
+    x = ra.rapid_norm_modulate(x, torch.full_like(x, NAN))
+    want = lo.norm_modulate(widen(normal((5, C), 71)))
+    assert_within(x[0, rows], want, modulate_bound(widen(normal((5, C), 71)), None, want))
+    x[0, rows] = 0
+    assert not x.any()
+    del x
+    H, n, D = 24, 700000, 128                                                      # 4.3 GB each of q and k
+    t = torch.zeros((2, 1, H, n, D), dtype=torch.bfloat16, device="cuda")
+    at = [(0, 0), (7, 599186), (23, n - 1), (12, 1), (11, n - 2)]
+    u = normal((5, 2, D), 72, 2.0)
+    for (h, r), v in zip(at, u):
+        t[:, 0, h, r] = v
+    table = torch.zeros((n, 64, 2), device="cuda")
+    some = angles(5, 128, 73)
+    for (h, r), v in zip(at, some):
+        table[r] = v
+    q, k = ra.rapid_qk_norm_rope([(t[0], t[1], t[0], t[1])], None, table)
+    for (h, r), v, a in zip(at, widen(u), widen(some)):
+        for got, one in zip((q, k), v):
+            want = lo.rotate(lo.head_norm(one)[None, None, None], a[None], "interleaved")[0, 0, 0]
+            assert_within(got[0, h, r], want, row_bound(one, None, want, True, 128))
+
+
+def calls():
+    """Every operator as (call, its outputs), in ways that the native form takes and in ways that it leaves to Python's."""
+    x, w, g, r = normal((2, 9, 64), 1), normal((40, 64), 2, 0.1), normal((2, 40), 3), normal((2, 9, 40), 4)
+    b = normal((40,), 5)
+    out, y = torch.empty_like(r), torch.empty_like(x)
+    v = normal((2, 2, 64), 6)
+    q = normal((4, 2, 3, 9, 64), 7)
+    table = torch.empty(9, 32, 2, device="cuda")
+    p = torch.arange(9, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    axes = [ra.RopeAxis(64, 100.0, "ntk", 2.0)]
+    fixed = angles(9, 32, 8)
+    norms = [(normal((64,), 9), None)]
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    return [
+        (lambda: ra.rapid_linear(x, w, out, b, "silu", g, r), [out]), (lambda: ra.rapid_linear(x, w, out, workspace=ws), [out]),
+        (lambda: ra.rapid_linear(x[0], w, out[1], None, "gelu_tanh", g[1], r[0]), [out]),
+        (lambda: ra.rapid_norm_modulate(x, y, v[:, 0], v[:, 1]), [y]), (lambda: ra.rapid_norm_modulate(x[1], y[0], v[0, 0], v[0, 1], eps=0), [y]),
+        (lambda: ra.rapid_rope_table(p, axes, table), [table]), (lambda: ra.rapid_rope_table(p, iter(axes), table, magnitude=2), [table]),
+        (lambda: ra.rapid_rope([(q[0], q[1], q[2], q[3])], fixed, "half"), [q]),
+        (lambda: ra.rapid_rope(((q[0], q[1], q[2], q[3]),), fixed[None].repeat(2, 1, 1, 1)), [q]),
+        (lambda: ra.rapid_qk_norm_rope([[q[0], q[1], q[2], q[3]]], norms, fixed), [q]),
+        (lambda: ra.rapid_qk_norm_rope([(q[0], q[1], q[2], q[3])]), [q]),
+    ]
+
+
+def test_both_forms_of_the_binding_agree(monkeypatch):
+    results = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(ra.binding, "_native", ra.binding._NoNative())
+        results.append([])
+        for call, outs in calls():
+            call()
+            results[-1] += [t.clone() for t in outs]
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and len(results[0]) == 11
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals_of_tensors_that_do_not_fit(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(ra.binding, "_native", ra.binding._NoNative())
+    x, w, out = normal((2, 9, 64), 1), normal((40, 64), 2), torch.empty((2, 9, 40), dtype=torch.bfloat16, device="cuda")
+    q = normal((1, 2, 9, 64), 3)
+    table = angles(9, 64, 1)
+    p = torch.zeros((9, 1), dtype=torch.int32, device="cuda")
+    refused = [
+        (TypeError, lambda: ra.rapid_linear(x.float(), w, out)), (TypeError, lambda: ra.rapid_linear(x, w.cpu(), out)),
+        (TypeError, lambda: ra.rapid_linear(x, w, out, b"bias")), (TypeError, lambda: ra.rapid_linear(x[:, :, ::2], w[:, :32], out)),
+        (ValueError, lambda: ra.rapid_linear(x, w[:, :56], out)), (ValueError, lambda: ra.rapid_linear(x, w, out[:1])),
+        (ValueError, lambda: ra.rapid_linear(x, w, out, w[0])), (ValueError, lambda: ra.rapid_linear(x, w, out, activation="relu")),
+        (ValueError, lambda: ra.rapid_linear(x, w, out, gate=out[0])), (ValueError, lambda: ra.rapid_linear(x, w, out, residual=out[:, :8])),
+        (TypeError, lambda: ra.rapid_linear(x, w, out, workspace=4)), (ra.RapidAttnError, lambda: ra.rapid_linear(x[..., :60], w[:, :60], out)),
+        (ra.RapidAttnError, lambda: ra.rapid_linear(x, w, out[:, :1].expand(2, 9, 40))),
+        (ValueError, lambda: ra.rapid_norm_modulate(x, x, w[0])), (ValueError, lambda: ra.rapid_norm_modulate(x, x[:, :8])),
+        (ra.RapidAttnError, lambda: ra.rapid_norm_modulate(x[..., 1:57], x[..., 1:57])),
+        (TypeError, lambda: ra.rapid_rope_table(p.long(), [ra.RopeAxis(64)], table)), (ValueError, lambda: ra.rapid_rope_table(p, [ra.RopeAxis(32)], table)),
+        (ValueError, lambda: ra.rapid_rope_table(p, [ra.RopeAxis(64)] * 2, table)), (ra.RapidAttnError, lambda: ra.rapid_rope_table(p, [ra.RopeAxis(64, -1.0)], table)),
+        (ValueError, lambda: ra.rapid_rope([(q, q, q, q)], table[:8])), (ra.RapidAttnError, lambda: ra.rapid_rope([(q, q, q, q)], table)),
+        (ValueError, lambda: ra.rapid_rope([(q, q[:, :1], q, q)], table)), (TypeError, lambda: ra.rapid_rope([(q, q, q, q)], table.half())),
+        (ValueError, lambda: ra.rapid_qk_norm_rope([(q, q, q, q)], [])), (ValueError, lambda: ra.rapid_qk_norm_rope([(q, q, q, q)], [(w[0, :32].contiguous(), None)])),
+    ]
+    for kind, call in refused:
+        with pytest.raises(kind):
+            call()

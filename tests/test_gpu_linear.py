@@ -145,3 +145,73 @@ def test_whole_numbers_are_exact():
         w = torch.from_numpy(rng.integers(-1, 2, (N, K)).astype(np.float32)).to(torch.bfloat16).cuda()
         got = ra.rapid_linear(x, w, torch.empty((n, N), dtype=torch.bfloat16, device="cuda"))
         np.testing.assert_array_equal(widen(got), widen(x) @ widen(w).T)
+
+
+# (one of each tile: 256 x 192, 256 x 160, 256 x 256, 128 x 128 in pieces and whole; several tiles a workgroup; ends of K and N inside)
+LARGE = [(2, 4000, 1544, 4600), (1, 8191, 3000, 2431), (2, 20000, 200, 1000), (1, 1024, 6144, 1536), (3, 1000, 1000, 2500), (1, 16000, 512, 4097),
+         (40, 201, 264, 2000), (9000, 1, 704, 1500)]
+
+
+@pytest.mark.parametrize("size", LARGE, ids=str)
+@pytest.mark.parametrize("gated", [False, True])
+def test_large(size, gated):
+    B, n, K, N = size
+    g = torch.Generator("cuda").manual_seed(sum(size))
+
+    def make(*shape, scale=1.0):
+        return (torch.randn(shape, generator=g, device="cuda") * scale).to(torch.bfloat16)
+
+    x, w, b = inside(make(B, n, K), 1, 2, 8)[0], make(N, K, scale=K ** -0.5), make(N, scale=0.3)
+    gate, res = (make(B, N), make(B, n, N)) if gated else (None, None)
+    out, big = inside(torch.full((B, n, N), NAN, dtype=torch.bfloat16, device="cuda"), 1, 1, 3)
+    ra.rapid_linear(x, w, out, b, "gelu_tanh" if gated else "none", gate, res)
+    assert torch.isfinite(out).all() and untouched_around(out, big)
+    m = np.unique(np.concatenate([[0, B * n - 1], np.random.default_rng(1).integers(0, B * n, 300), np.arange(max(0, B * n - 260), B * n, 37)]))
+    s, r = torch.from_numpy(m // n).cuda(), torch.from_numpy(m % n).cuda()
+    rows = [widen(t) for t in (x[s, r], w, b)] + ([widen(gate[s]), widen(res[s, r])] if gated else [None, None])
+    act = "gelu_tanh" if gated else "none"
+    args = (rows[0][:, None], rows[1], rows[2], act, rows[3], None if rows[4] is None else rows[4][:, None])
+    want = lo.linear(*args)
+    assert_within(out[s, r][:, None], want, bound(*args, want), str(size))
+
+
+def test_samples_shorter_than_a_tile():
+    """A gate of its own for every sample, many samples in one tile of rows."""
+    check(40, 7, 192, 192, "silu", True, True, True, seed=31)
+    check(300, 1, 136, 72, "none", True, True, True, seed=32)
+    check(9, 30, 2432, 100, "gelu_tanh", False, True, True, seed=33)
+
+
+def test_offsets_beyond_32_bits():
+    """x and y of more than 2^32 bytes each, w of rows far apart."""
+    n, K, N = 300000, 8192, 8000
+    x = torch.zeros((n, K), dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 1, 131071, 262143, 262144, 299998, 299999], device="cuda")
+    x[rows] = normal((7, K), 41)
+    w = torch.full((N, 8200), NAN, dtype=torch.bfloat16, device="cuda")[:, :K]
+    w.copy_(normal((N, K), 42, K ** -0.5))
+    out = torch.full((n, N), NAN, dtype=torch.bfloat16, device="cuda")
+    ra.rapid_linear(x, w, out)
+    args = (widen(x[rows])[None], widen(w))
+    want = lo.linear(*args)
+    assert_within(out[rows][None], want, bound(*args, None, "none", None, None, want))
+    out[rows] = 0
+    assert not out.any()                                                           # every other row of x is zero
+
+
+def test_without_a_workspace():
+    for B, n, K, N in ((1, 100, 2432, 100), (1, 1024, 6144, 1536)):
+        assert ra.rapid_linear_workspace_bytes(B * n, N, K) > 0
+        x, w = normal((n, K), 51), normal((N, K), 52, K ** -0.5)
+        out = torch.empty((n, N), dtype=torch.bfloat16, device="cuda")
+        rows = ra.binding.Rows(x.data_ptr(), 0, K), ra.binding.Rows(out.data_ptr(), 0, N)
+        status = ra.library().rapid_linear(rows[0], w.data_ptr(), K, None, rows[1], 0, None, 0, None, 1, n, N, K, None, 0,
+                                           torch.cuda.current_stream().cuda_stream)
+        assert status == 0
+        args = (widen(x)[None], widen(w))
+        want = lo.linear(*args)
+        assert_within(out[None], want, bound(*args, None, "none", None, None, want))
+        small = torch.empty(64, dtype=torch.uint8, device="cuda")
+        with pytest.raises(ra.RapidAttnError) as e:
+            ra.rapid_linear(x, w, out, workspace=small)
+        assert e.value.status == ra.STATUS["RAPID_ERR_WORKSPACE"]
