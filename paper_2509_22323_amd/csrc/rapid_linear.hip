@@ -207,7 +207,9 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         asm volatile("" : "+v"(l));
         return l;
     };
-    auto chunk_of = [](int lane) { return (unsigned)((lane & 7) ^ (lane >> 3)); };    // the row's 16 bytes that a lane fetches
+    // A row's 16-byte chunk c lies at c ^ (row / 2 % 8), so that the 16 rows that are read at a time are in different banks: the
+    // chunk that a lane fetches in the copy of rows 8 i .. 8 i + 7.
+    auto chunk_of = [](int lane, int i) { return (lane & 7) ^ ((i & 1) << 2 | lane >> 4); };
     auto sources_x = [&] {
         int r0;
         const int lane = lane_here();
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         for (int i = 0; i < XC; ++i) {
             int b, r;
             sample_of(p, min(m0 + (wave * XC + i) * 8 + (lane >> 3), p.M - 1), b, r);
-            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk_of(lane) * 16u;
+            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk_of(lane, wave * XC + i) * 16u;
         }
     };
     auto sources_w = [&] {
@@ -229,13 +231,14 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         wplace = turn;
 #pragma unroll
         for (int i = 0; i < WALL; ++i)
-            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk_of(lane) * 16u;
+            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk_of(lane, wfirst + i) * 16u;
     };
-    auto mask = [&](int step, auto& off) {             // zeros for what lies behind the rows' ends
+    auto mask = [&](int step, int i, auto& off) {      // zeros for what lies behind the rows' ends (i: the first copy)
         const int left = p.K - (first + step) * STEP;
         if (left >= STEP) return;
-        if ((int)chunk_of(lane_here()) * 8 >= left)
-            for (unsigned& o : off) o = NOWHERE;
+        const int lane = lane_here();
+        for (unsigned& o : off)
+            if (chunk_of(lane, i++) * 8 >= left) o = NOWHERE;
     };
     int xrecords = (int)BUFFER, wrecords = (int)BUFFER;
     auto copy_x = [&](int slot, int c) { copy_1k(xbase, xrecords, xoff[c], (unsigned)(size_t)(lds_char*)lds + slot * XB + (wave * XC + c) * 1024); };
@@ -250,7 +253,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
 
     // Fragments: lane (i, g) of 16 x 4 has row i's inputs 8 g .. 8 g + 7 of 32; the second half of a step is 64 bytes on.
     const int wm = wave >> 1, wn = wave & 1;
-    const unsigned in_row = (unsigned)((lane & 15) * ROW + (((lane >> 4) ^ (lane & 7)) << 4));
+    const unsigned in_row = (unsigned)((lane & 15) * ROW + (((lane >> 4) ^ (lane >> 1 & 7)) << 4));
     const unsigned xat = in_row + wm * (16 * FM * ROW), wat = in_row + XS * XB + wn * (16 * FN * ROW);
     bf16x8 xf[2][FM], wf[2][FN];
     auto fetch_one = [&](int xslot, int wslot, int half, int r, bf16x8 (&x)[FM], bf16x8 (&w)[FN]) {
@@ -297,13 +300,13 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
         if (i < XS) {
-            mask(i, xoff);
+            mask(i, wave * XC, xoff);
 #pragma unroll
             for (int c = 0; c < XC; ++c) copy_x(i, c);
             on(xbase, xplace);
         }
         if (i < WS) {
-            mask(i, woff);
+            mask(i, wfirst, woff);
 #pragma unroll
             for (int c = 0; c < WALL; ++c) copy_w(i, c);
             on(wbase, wplace);
@@ -339,8 +342,8 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
                 if (more) sources_w();
                 else wrecords = 0;
             }
-            mask(xnext, xoff);
-            mask(wnext, woff);
+            mask(xnext, wave * XC, xoff);
+            mask(wnext, wfirst, woff);
             half_step(xf[0], wf[0], [&](int r) { fetch_one(xslot, wslot, 1, r, xf[1], wf[1]); }, [](int) {});
             // Everyone has read this step, and the next one has arrived; what the deeper buffer gets, last in a step, has a step
             // more.  (Behind an item's results everything is awaited: stores are counted too.)
