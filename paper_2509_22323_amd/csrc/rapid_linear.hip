@@ -120,18 +120,26 @@ constexpr int ROW = STEP * 2;
 constexpr int CUS = 256;
 constexpr int MOST_PIECES = 8;                         // along K
 constexpr unsigned NOWHERE = 0xC0000000u;              // an offset outside any buffer below
-constexpr unsigned BUFFER = 0x80000100u;               // bytes that a tile's rows may span
+constexpr unsigned BUFFER = 0x81000000u;               // bytes that a tile's rows may span, and the inputs of a row
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
-// 1 KB from 64 lanes' addresses into LDS: lane i's 16 bytes go to dst + 16 i.  Assembly, so that only the waits below order it
-// (a wait state between the scalar write of M0 and the copy).
-__device__ __forceinline__ void copy_1k(unsigned long long base, int records, unsigned off, unsigned dst)
+// 1 KB from 64 lanes' addresses into LDS: lane i's 16 bytes go to dst + 1024 C + 16 i.  (The instruction's offset counts on both
+// sides: LESS is taken off the lanes' offsets.)  Assembly, so that only the waits below order it; a wait state between the scalar
+// write of M0 and the copy.
+constexpr unsigned LESS = 3072;
+template <int C>
+__device__ __forceinline__ void copy_1k(const i32x4& buffer, unsigned off, int at, unsigned dst)
 {
-    const i32x4 rsrc = {(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), records, 0x00020000};
-    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(rsrc));
+    static_assert(C >= 0 && C < 4, "an offset of 12 bits");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen offset:%4 lds" ::"{m0}"(dst), "v"(off), "s"(buffer), "s"(at), "i"(1024 * C));
+}
+__device__ __forceinline__ i32x4 buffer_at(const void* p)
+{
+    const unsigned long long base = (unsigned long long)p - LESS;
+    return i32x4{(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), (int)BUFFER, 0x00020000};
 }
 
 // s_waitcnt vmcnt(VM) lgkmcnt(0), then the barrier; nothing moves across.
@@ -183,11 +191,13 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     const int mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN, all_steps = (p.K + STEP - 1) / STEP;
 
     // Where the tile's copies come from.  Its first sample is the base of its x rows (its first row where there is one sample).
-    int m0, j0, b0, piece = 0, first = 0, steps = max(all_steps, MOST), xplace, wplace;
+    int m0, j0, b0, piece = 0, first = 0, steps = max(all_steps, MOST);
     // Rows lie a multiple of many memory channels apart, so the same step of all of them lies in few channels: every XCD begins
     // at another step and comes round to those before it (its workgroups stay together, they share what its L2 holds).
     const int turn = !SPLIT && all_steps >= 8 && p.K % STEP == 0 ? (int)(blockIdx.x % 8) * all_steps / 8 : 0;
-    unsigned long long xbase, wbase;
+    const bool ragged = p.K % STEP != 0 || all_steps < MOST;
+    i32x4 xbuffer, wbuffer;
+    int xk, wk;                                        // bytes of a row before the step that is copied next
     unsigned xoff[XC], woff[WALL];
     auto locate = [&](int id) {
         int mi, ni, t = turn_of(id, items);
@@ -216,39 +226,39 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         sample_of(p, m0, b0, r0);
         b0 = __builtin_amdgcn_readfirstlane(b0);
         r0 = __builtin_amdgcn_readfirstlane(r0);
-        xbase = (unsigned long long)(p.x + b0 * p.x_sb + (one ? (long long)r0 * p.x_sn : 0)) + (first + turn) * ROW;
-        xplace = turn;
+        xbuffer = buffer_at(p.x + b0 * p.x_sb + (one ? (long long)r0 * p.x_sn : 0));
+        xk = (first + turn) * ROW;
 #pragma unroll
         for (int i = 0; i < XC; ++i) {
             int b, r;
             sample_of(p, min(m0 + (wave * XC + i) * 8 + (lane >> 3), p.M - 1), b, r);
-            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk_of(lane, wave * XC + i) * 16u;
+            xoff[i] = (unsigned)(b - b0) * (unsigned)(p.x_sb * 2) + (unsigned)(one ? r - r0 : r) * (unsigned)(p.x_sn * 2) + chunk_of(lane, wave * XC + i) * 16u + (LESS - 1024u * i);
         }
     };
     auto sources_w = [&] {
         const int lane = lane_here();
-        wbase = (unsigned long long)(p.w + (long long)j0 * p.w_sn) + (first + turn) * ROW;
-        wplace = turn;
+        wbuffer = buffer_at(p.w + (long long)j0 * p.w_sn);
+        wk = (first + turn) * ROW;
 #pragma unroll
         for (int i = 0; i < WALL; ++i)
-            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk_of(lane, wfirst + i) * 16u;
+            woff[i] = (unsigned)min((wfirst + i) * 8 + (lane >> 3), p.N - 1 - j0) * (unsigned)(p.w_sn * 2) + chunk_of(lane, wfirst + i) * 16u + (LESS - 1024u * i);
     };
-    auto mask = [&](int step, int i, auto& off) {      // zeros for what lies behind the rows' ends (i: the first copy)
-        const int left = p.K - (first + step) * STEP;
-        if (left >= STEP) return;
+    auto mask = [&](int k, int i, auto& off) {         // zeros for what lies behind the rows' ends (i: the first copy)
+        const int left = 2 * p.K - k;
+        if (left >= ROW) return;
         const int lane = lane_here();
         for (unsigned& o : off)
-            if (chunk_of(lane, i++) * 8 >= left) o = NOWHERE;
+            if (chunk_of(lane, i++) * 16 >= left) o = NOWHERE;
     };
-    int xrecords = (int)BUFFER, wrecords = (int)BUFFER;
-    auto copy_x = [&](int slot, int c) { copy_1k(xbase, xrecords, xoff[c], (unsigned)(size_t)(lds_char*)lds + slot * XB + (wave * XC + c) * 1024); };
-    auto copy_w = [&](int slot, int c) {
-        if (c < WC || wave < WREST) copy_1k(wbase, wrecords, woff[c], (unsigned)(size_t)(lds_char*)lds + XS * XB + slot * WB + (wfirst + c) * 1024);
+    static_assert(XC <= 4 && WALL <= 4, "");
+    const unsigned lds_at = (unsigned)(size_t)(lds_char*)lds, xdst = lds_at + wave * XC * 1024, wdst = lds_at + XS * XB + wfirst * 1024;
+    auto copy_x = [&](int slot, auto c) { copy_1k<c.value>(xbuffer, xoff[c.value], xk, xdst + slot); };
+    auto copy_w = [&](int slot, auto c) {
+        if (c.value < WC || wave < WREST) copy_1k<c.value>(wbuffer, woff[c.value], wk, wdst + slot);
     };
-    auto on = [&](unsigned long long& base, int& place) {
-        const bool round = ++place == steps;
-        base += round ? ROW - steps * ROW : ROW;
-        place = round ? 0 : place;
+    auto on = [&](int& k) {                            // round to the item's first step behind its last
+        k += ROW;
+        k = k == (first + steps) * ROW ? first * ROW : k;
     };
 
     // Fragments: lane (i, g) of 16 x 4 has row i's inputs 8 g .. 8 g + 7 of 32; the second half of a step is 64 bytes on.
@@ -257,24 +267,33 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     const unsigned xat = in_row + wm * (16 * FM * ROW), wat = in_row + XS * XB + wn * (16 * FN * ROW);
     bf16x8 xf[2][FM], wf[2][FN];
     auto fetch_one = [&](int xslot, int wslot, int half, int r, bf16x8 (&x)[FM], bf16x8 (&w)[FN]) {
-        if (r < FM) x[r] = *(lds_bf16x8*)((lds_char*)lds + xslot * XB + (xat ^ (half * 64)) + r * 16 * ROW);
-        else w[r - FM] = *(lds_bf16x8*)((lds_char*)lds + wslot * WB + (wat ^ (half * 64)) + (r - FM) * 16 * ROW);
+        if (r < FM) x[r] = *(lds_bf16x8*)((lds_char*)lds + xslot + (xat ^ (half * 64)) + r * 16 * ROW);
+        else w[r - FM] = *(lds_bf16x8*)((lds_char*)lds + wslot + (wat ^ (half * 64)) + (r - FM) * 16 * ROW);
     };
     f32x4 acc[FN][FM];
+    // Calls f with the numbers A .. B - 1 as constants.
+    auto each = [](auto a, auto b, auto&& f) {
+        auto go = [&](auto self, auto i) {
+            if constexpr (i.value < b.value) {
+                f(i);
+                self(self, std::integral_constant<int, i.value + 1>());
+            }
+        };
+        go(go, a);
+    };
     // Half a step: FN blocks of FM MFMAs, each behind its share of the reads for the next half and of the copies for a step
     // to come.
     auto half_step = [&](const bf16x8 (&x)[FM], const bf16x8 (&w)[FN], auto&& read, auto&& put) {
         constexpr int READS = FM + FN, FIRST = FN > 2 ? FN - 2 : 1;          // the last blocks' MFMAs cover the last reads
-#pragma unroll
-        for (int i = 0; i < FN; ++i) {
+        each(std::integral_constant<int, 0>(), std::integral_constant<int, FN>(), [&](auto block) {
+            constexpr int i = block.value;
 #pragma unroll
             for (int r = i * READS / FIRST; r < (i + 1) * READS / FIRST && r < READS; ++r) read(r);
-#pragma unroll
-            for (int c = i * COPIES / FN; c < (i + 1) * COPIES / FN; ++c) put(c);
+            each(std::integral_constant<int, i * COPIES / FN>(), std::integral_constant<int, (i + 1) * COPIES / FN>(), put);
 #pragma unroll
             for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i], x[j], acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     };
     // A lane's sums begin with the bias of its four columns of each fragment.
     bf16x4 bias[FN] = {};
@@ -300,16 +319,14 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
         if (i < XS) {
-            mask(i, wave * XC, xoff);
-#pragma unroll
-            for (int c = 0; c < XC; ++c) copy_x(i, c);
-            on(xbase, xplace);
+            if (ragged) mask(xk, wave * XC, xoff);
+            each(std::integral_constant<int, 0>(), std::integral_constant<int, XC>(), [&](auto c) { copy_x(i * XB, c); });
+            on(xk);
         }
         if (i < WS) {
-            mask(i, wfirst, woff);
-#pragma unroll
-            for (int c = 0; c < WALL; ++c) copy_w(i, c);
-            on(wbase, wplace);
+            if (ragged) mask(wk, wfirst, woff);
+            each(std::integral_constant<int, 0>(), std::integral_constant<int, WALL>(), [&](auto c) { copy_w(i * WB, c); });
+            on(wk);
         }
     }
     arrive<0>();
@@ -327,38 +344,41 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         const int length = steps;
         // A step's buffer is free once its second half is in registers: the step XS (WS) on goes there during the multiplication of
         // that half; behind the last steps the first ones of this workgroup's next item, or nothing (a buffer without bytes).
-        for (int left = steps, xnext = XS, wnext = WS; left > 0; --left, ++xnext, ++wnext) {
-            if (left == MOST && more) {
-                id += gridDim.x;
-                locate(id);
+        for (int left = steps; left > 0; --left) {
+            if (left <= MOST) {
+                if (left == MOST && more) {
+                    id += gridDim.x;
+                    locate(id);
+                }
+                if (left == XS) {
+                    if (more) sources_x();
+                    else xbuffer[2] = 0;
+                }
+                if (left == WS) {
+                    if (more) sources_w();
+                    else wbuffer[2] = 0;
+                }
             }
-            if (left == XS) {
-                xnext = 0;
-                if (more) sources_x();
-                else xrecords = 0;
+            if (ragged) {
+                mask(xk, wave * XC, xoff);
+                mask(wk, wfirst, woff);
             }
-            if (left == WS) {
-                wnext = 0;
-                if (more) sources_w();
-                else wrecords = 0;
-            }
-            mask(xnext, wave * XC, xoff);
-            mask(wnext, wfirst, woff);
-            half_step(xf[0], wf[0], [&](int r) { fetch_one(xslot, wslot, 1, r, xf[1], wf[1]); }, [](int) {});
+            half_step(xf[0], wf[0], [&](int r) { fetch_one(xslot, wslot, 1, r, xf[1], wf[1]); }, [](auto) {});
             // Everyone has read this step, and the next one has arrived; what the deeper buffer gets, last in a step, has a step
             // more.  (Behind an item's results everything is awaited: stores are counted too.)
             if (left < length) arrive<LATE>();
             else arrive<0>();
             const int xfree = xslot, wfree = wslot;
-            xslot = xslot == XS - 1 ? 0 : xslot + 1;
-            wslot = wslot == WS - 1 ? 0 : wslot + 1;
-            half_step(xf[1], wf[1], [&](int r) { fetch_one(xslot, wslot, 0, r, xf[0], wf[0]); }, [&](int c) {
-                if constexpr (XS > WS) c < WALL ? copy_w(wfree, c) : copy_x(xfree, c - WALL);
-                else c < XC ? copy_x(xfree, c) : copy_w(wfree, c - XC);
+            xslot = xslot == (XS - 1) * XB ? 0 : xslot + XB;
+            wslot = wslot == (WS - 1) * WB ? 0 : wslot + WB;
+            half_step(xf[1], wf[1], [&](int r) { fetch_one(xslot, wslot, 0, r, xf[0], wf[0]); }, [&](auto c) {
+                constexpr int X0 = XS > WS ? WALL : 0, W0 = XS > WS ? 0 : XC;
+                if constexpr (c.value >= X0 && c.value < X0 + XC) copy_x(xfree, std::integral_constant<int, c.value - X0>());
+                else copy_w(wfree, std::integral_constant<int, c.value - W0>());
             });
             asm volatile("" ::: "memory");
-            on(xbase, xplace);
-            on(wbase, wplace);
+            on(xk);
+            on(wk);
         }
 
         const int lane = lane_here();
