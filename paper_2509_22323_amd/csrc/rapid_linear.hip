@@ -182,8 +182,13 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     constexpr int XS = BOTH || WR == 4 ? 3 : 2, WS = BOTH || WR < 4 ? 3 : 2, MOST = 3;
     static_assert(XS * XB + WS * WB <= 160 * 1024 / PER_CU, "");
     constexpr int XC = TM / 8 / WAVES, WC = TN / 8 / WAVES, WREST = TN / 8 % WAVES;    // copies of a wavefront: of x; of w, and one more for some
-    constexpr int WALL = WC + (WREST ? 1 : 0), COPIES = XC + WALL;
-    constexpr int LATE = BOTH ? XC + WC : XS > WS ? XC : WC;          // copies that may be on their way yet when a step begins
+    constexpr int WALL = WC + (WREST ? 1 : 0);
+    // The copies are spread over the two halves of a step (a CU's memory pipeline takes 16 cycles for each): those of the deeper
+    // buffer, for two steps on, go with the first half, the other operand's with the second.
+    constexpr bool X_FIRST = XS == 3;
+    constexpr int FIRST = X_FIRST ? XC : WALL, SECOND = X_FIRST ? WALL : XC;
+    constexpr int XA = X_FIRST ? 2 : XS, WA = X_FIRST ? WS : 2;       // steps ahead at which x and w are copied
+    constexpr int LATE = BOTH ? XC + WC : X_FIRST ? XC : WC;          // copies that may be on their way yet when a step begins
     __shared__ __align__(1024) char lds[XS * XB + WS * WB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool one = p.n == p.M;
@@ -283,12 +288,12 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     };
     // Half a step: FN blocks of FM MFMAs, each behind its share of the reads for the next half and of the copies for a step
     // to come.
-    auto half_step = [&](const bf16x8 (&x)[FM], const bf16x8 (&w)[FN], auto&& read, auto&& put) {
-        constexpr int READS = FM + FN, FIRST = FN > 2 ? FN - 2 : 1;          // the last blocks' MFMAs cover the last reads
+    auto half_step = [&](const bf16x8 (&x)[FM], const bf16x8 (&w)[FN], auto&& read, auto copies, auto&& put) {
+        constexpr int READS = FM + FN, READING = FN > 2 ? FN - 2 : 1, COPIES = copies.value;    // the last blocks' MFMAs cover the last reads
         each(std::integral_constant<int, 0>(), std::integral_constant<int, FN>(), [&](auto block) {
             constexpr int i = block.value;
 #pragma unroll
-            for (int r = i * READS / FIRST; r < (i + 1) * READS / FIRST && r < READS; ++r) read(r);
+            for (int r = i * READS / READING; r < (i + 1) * READS / READING && r < READS; ++r) read(r);
             each(std::integral_constant<int, i * COPIES / FN>(), std::integral_constant<int, (i + 1) * COPIES / FN>(), put);
 #pragma unroll
             for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i], x[j], acc[i][j], 0, 0, 0);
@@ -318,12 +323,12 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     sources_w();
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
-        if (i < XS) {
+        if (i < XA) {
             if (ragged) mask(xk, wave * XC, xoff);
             each(std::integral_constant<int, 0>(), std::integral_constant<int, XC>(), [&](auto c) { copy_x(i * XB, c); });
             on(xk);
         }
-        if (i < WS) {
+        if (i < WA) {
             if (ragged) mask(wk, wfirst, woff);
             each(std::integral_constant<int, 0>(), std::integral_constant<int, WALL>(), [&](auto c) { copy_w(i * WB, c); });
             on(wk);
@@ -342,19 +347,19 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_end = min(m0 + TM, p.M);
         const bool more = id + (int)gridDim.x < items;
         const int length = steps;
-        // A step's buffer is free once its second half is in registers: the step XS (WS) on goes there during the multiplication of
-        // that half; behind the last steps the first ones of this workgroup's next item, or nothing (a buffer without bytes).
+        // A step's buffer is free once its second half is in registers; behind the last steps follow the first ones of this
+        // workgroup's next item, or nothing (a buffer without bytes).
         for (int left = steps; left > 0; --left) {
             if (left <= MOST) {
-                if (left == MOST && more) {
+                if (left == (XA > WA ? XA : WA) && more) {
                     id += gridDim.x;
                     locate(id);
                 }
-                if (left == XS) {
+                if (left == XA) {
                     if (more) sources_x();
                     else xbuffer[2] = 0;
                 }
-                if (left == WS) {
+                if (left == WA) {
                     if (more) sources_w();
                     else wbuffer[2] = 0;
                 }
@@ -363,18 +368,21 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
                 mask(xk, wave * XC, xoff);
                 mask(wk, wfirst, woff);
             }
-            half_step(xf[0], wf[0], [&](int r) { fetch_one(xslot, wslot, 1, r, xf[1], wf[1]); }, [](auto) {});
-            // Everyone has read this step, and the next one has arrived; what the deeper buffer gets, last in a step, has a step
-            // more.  (Behind an item's results everything is awaited: stores are counted too.)
+            const int before = X_FIRST ? (xslot == 0 ? (XS - 1) * XB : xslot - XB) : (wslot == 0 ? (WS - 1) * WB : wslot - WB);
+            half_step(xf[0], wf[0], [&](int r) { fetch_one(xslot, wslot, 1, r, xf[1], wf[1]); }, std::integral_constant<int, FIRST>(), [&](auto c) {
+                if constexpr (X_FIRST) copy_x(before, c);
+                else copy_w(before, c);
+            });
+            // Everyone has read this step, and the next one has arrived.  (Behind an item's results everything is awaited: stores
+            // are counted too.)
             if (left < length) arrive<LATE>();
             else arrive<0>();
             const int xfree = xslot, wfree = wslot;
             xslot = xslot == (XS - 1) * XB ? 0 : xslot + XB;
             wslot = wslot == (WS - 1) * WB ? 0 : wslot + WB;
-            half_step(xf[1], wf[1], [&](int r) { fetch_one(xslot, wslot, 0, r, xf[0], wf[0]); }, [&](auto c) {
-                constexpr int X0 = XS > WS ? WALL : 0, W0 = XS > WS ? 0 : XC;
-                if constexpr (c.value >= X0 && c.value < X0 + XC) copy_x(xfree, std::integral_constant<int, c.value - X0>());
-                else copy_w(wfree, std::integral_constant<int, c.value - W0>());
+            half_step(xf[1], wf[1], [&](int r) { fetch_one(xslot, wslot, 0, r, xf[0], wf[0]); }, std::integral_constant<int, SECOND>(), [&](auto c) {
+                if constexpr (X_FIRST) copy_w(wfree, c);
+                else copy_x(xfree, c);
             });
             asm volatile("" ::: "memory");
             on(xk);
