@@ -592,17 +592,17 @@ struct Plan {
 // What a product takes, in us.  Its items (tiles times pieces) go to 256 CUs with each slots of them at a time: full rounds, whose
 // steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full`; every round
 // has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.  Pieces are added up by a second kernel,
-// which costs `join` and `sum` for every million numbers that it reads.  Fitted to 600 products of 5 to 32768 rows, 16 to 9728
+// which costs `join` and `sum` for every million numbers that it reads.  Fitted to 800 products of 5 to 32768 rows, 16 to 9728
 // outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8 pieces, inputs changing
-// from call to call: the plan found by it takes 1.014 times what the best one does in the geometric mean (1.37 times at most).
+// from call to call: the plan found by it takes 1.013 times what the best one does in the geometric mean (1.37 times at most).
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;
 };
 constexpr TileCost COST[TILES] = {
-    {64, 64, 4, 0.357f, 0.930f, 2.05f, 0.64f, 2.46f, 2.22f, 2.27f}, {128, 128, 2, 0.464f, 1.189f, 3.65f, 0.61f, 2.44f, 2.05f, 1.54f},
-    {256, 160, 1, 0.712f, 1.230f, 5.40f, 0.76f, 1.85f, 0.f, 0.f},   {256, 192, 1, 0.791f, 1.351f, 6.05f, 0.79f, 1.54f, 0.f, 0.f},
-    {256, 256, 1, 1.042f, 1.757f, 7.30f, 0.86f, 1.57f, 0.f, 0.f}};
+    {64, 64, 4, 0.352f, 0.887f, 2.38f, 0.51f, 2.21f, 1.36f, 2.46f}, {128, 128, 2, 0.439f, 1.119f, 3.97f, 0.63f, 1.92f, 1.23f, 1.94f},
+    {256, 160, 1, 0.660f, 1.115f, 5.84f, 0.75f, 1.36f, 0.f, 0.f},   {256, 192, 1, 0.796f, 1.378f, 5.96f, 0.80f, 1.56f, 0.f, 0.f},
+    {256, 256, 1, 0.994f, 1.765f, 7.21f, 0.84f, 1.59f, 0.f, 0.f}};
 
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
