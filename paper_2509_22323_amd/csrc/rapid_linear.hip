@@ -487,9 +487,12 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
 
 // ---------------------------------------------------------------------------
 // A handful of rows (the conditioning's projections): MAX_M of x at most.  A wavefront takes OUT outputs of all rows and reads their
-// rows of w end to end, 1 KB an access; two products an instruction, the lanes' sums are added at the end.
+// rows of w end to end, 1 KB an access; two products an instruction, the lanes' sums are added at the end.  Bound by the bytes of w:
+// 2 rows, 1536 -> 9216 (28 MB): 4.7 us = 6.0 TB/s where w is in the caches, 6.9 us = 4.1 TB/s where w changes
+// from call to call; four outputs a wavefront and four wavefronts a workgroup, whose number then does not go evenly over the CUs:
+// 4.9 and 7.2, and 9.2 instead of 5.3 us for 4 rows, 9728 -> 100.
 // ---------------------------------------------------------------------------
-constexpr int OUT = 4, DOT_WAVES = 4, DOT_ROWS = 4;
+constexpr int OUT = 2, DOT_WAVES = 2;
 
 template <int MAX_M>
 __global__ __launch_bounds__(DOT_WAVES * 64) void linear_dot_kernel(LinearParams p)
@@ -555,6 +558,10 @@ __global__ __launch_bounds__(DOT_WAVES * 64) void linear_dot_kernel(LinearParams
     if (p.residual) mine += (float)p.residual[b * p.r_sb + (long long)r * p.r_sn + n];
     p.y[b * p.y_sb + (long long)r * p.y_sn + n] = (__bf16)mine;
 }
+
+// Every wavefront reads all of x.  Five to eight rows: 9.9 us here, 11.6 in tiles of matrix instructions at 1536 -> 9216, 8.8 / 11.6 at
+// 6144 -> 1536, but 20.5 / 16.7 at 2432 -> 14592.
+bool by_dots(long long M, int N, int K) { return M <= 4 || (M <= 8 && (long long)N * K <= 1 << 24); }
 
 template <int MAX_M>
 int launch_dot(const LinearParams& p, void* stream)
@@ -657,7 +664,7 @@ extern "C" {
 
 size_t rapid_linear_workspace_bytes(long long M, int N, int K)
 {
-    if (M <= DOT_ROWS || M >= (1LL << 31) - 256 || N <= 0 || N > MAX_STRIDE || K <= 0 || K > MAX_STRIDE || K % 8 != 0) return 0;
+    if (M <= 0 || M >= (1LL << 31) - 256 || N <= 0 || N > MAX_STRIDE || K <= 0 || K > MAX_STRIDE || K % 8 != 0 || by_dots(M, N, K)) return 0;
     const int pieces = plan_for(M, N, K, MOST_PIECES).pieces;
     return pieces > 1 ? (size_t)pieces * M * ((N + 7) / 8 * 8) * sizeof(float) : 0;
 }
@@ -698,7 +705,11 @@ int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const v
     p.K = K;
     p.activation = activation;
     if (B == 1) p.n = p.M;
-    if (M <= DOT_ROWS) return M == 1 ? launch_dot<1>(p, stream) : M == 2 ? launch_dot<2>(p, stream) : launch_dot<4>(p, stream);
+    if (by_dots(M, N, K)) {
+        if (M == 1) return launch_dot<1>(p, stream);
+        if (M == 2) return launch_dot<2>(p, stream);
+        return M <= 4 ? launch_dot<4>(p, stream) : launch_dot<8>(p, stream);
+    }
     const Plan plan = plan_for(M, N, K, workspace ? MOST_PIECES : 1);
     p.pieces = plan.pieces;
     p.pitch = (N + 7) / 8 * 8;

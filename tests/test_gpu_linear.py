@@ -70,6 +70,13 @@ def test_sizes(size):
     check(B, n, K, N, seed=sum(size))
 
 
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7, 8, 9])
+@pytest.mark.parametrize("K,N", [(8, 3), (512, 64), (1544, 131), (2560, 33), (6144, 1536)])
+def test_a_handful_of_rows(rows, K, N):
+    check(rows, 1, K, N, "silu", True, True, rows % 2 == 0, seed=rows)
+    check(1, rows, K, N, seed=rows)
+
+
 @pytest.mark.parametrize("act", ["none", "silu", "gelu_tanh"])
 @pytest.mark.parametrize("bias", [False, True])
 @pytest.mark.parametrize("gate,residual", [(False, False), (True, False), (False, True), (True, True)])
