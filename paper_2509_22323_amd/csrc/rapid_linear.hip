@@ -334,7 +334,8 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
             on(wk);
         }
     }
-    arrive<0>();
+    arrive<XC + WC + (BOTH ? WC : 0)>();               // (all but the steps behind the first)
+    bool stored = false;
     for (int xslot = 0, wslot = 0;;) {
 #pragma unroll
         for (int r = 0; r < FM + FN; ++r) fetch_one(xslot, wslot, 0, r, xf[0], wf[0]);
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
             for (int j = 0; j < FM; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) acc[i][j][q] = (float)bias[i][q];
-        const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_end = min(m0 + TM, p.M);
+        const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_end = min(m0 + TM, p.M), tile_right = j0 + TN;
         const bool more = id + (int)gridDim.x < items;
         const int length = steps;
         // A step's buffer is free once its second half is in registers; behind the last steps follow the first ones of this
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
             });
             // Everyone has read this step, and the next one has arrived.  (Behind an item's results everything is awaited: stores
             // are counted too.)
-            if (left < length) arrive<LATE>();
+            if (left < length || !stored) arrive<LATE>();
             else arrive<0>();
             const int xfree = xslot, wfree = wslot;
             xslot = xslot == (XS - 1) * XB ? 0 : xslot + XB;
@@ -407,49 +408,71 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         const bool one_sample = one || tile_end <= (first_sample + 1) * p.n;
         const int g = lane >> 4;
         constexpr int SIDE = FN / 2, UNITS = FM * SIDE, ALL = UNITS + (FN % 2) * FM / 2;
-        auto of = [&](int m, const __bf16* t, long long sb, int sn) {       // row m of a tensor
-            int b = first_sample, r = m - first_sample * p.n;
-            if (!one_sample) sample_of(p, m, b, r);
-            return t + b * sb + (long long)r * sn;
-        };
         auto row = [&](int u) { return mw + 16 * (u < UNITS ? u / SIDE : 2 * (u - UNITS) + (g & 1)) + (lane & 15); };
         auto column = [&](int u) { return nw + (u < UNITS ? 32 * (u % SIDE) + (g & 1) * 16 : 16 * (FN - 1)) + (g >> 1) * 8; };
-        constexpr int AHEAD = ALL < 6 ? ALL : 6;       // residuals on their way
-        bf16x8 gate[SIDE + 1] = {}, residual[AHEAD] = {};
-        auto load_residual = [&](int u) {
-            if (p.residual && row(u) < p.M && column(u) < p.N)
-                residual[u % AHEAD] = eight_of(of(row(u), p.residual, p.r_sb, p.r_sn), column(u), p.N);
+        // Smooth: one sample, and eight outputs or none wherever a lane writes.  Bare: neither activation, gate nor residual.  Most
+        // tiles need the smooth forms alone, which are short (one form for all cases, 7000 instructions long: 7 us a tile of
+        // 256 x 192).
+        auto results = [&](auto smooth, auto bare) {
+            constexpr bool SMOOTH = smooth.value, BARE = bare.value;
+            auto of = [&](int m, const __bf16* t, long long sb, int sn) {   // row m of a tensor
+                int b = first_sample, r = m - first_sample * p.n;
+                if (!SMOOTH && !one_sample) sample_of(p, m, b, r);
+                return t + b * sb + (long long)r * sn;
+            };
+            auto load = [&](const __bf16* at, int n) { return SMOOTH ? (bf16x8)*(const bf16x8_anywhere*)(at + n) : eight_of(at, n, p.N); };
+            constexpr int AHEAD = ALL < 6 ? ALL : 6;       // residuals on their way
+            bf16x8 gate[SIDE + 1] = {}, residual[AHEAD] = {};
+            auto load_residual = [&](int u) {
+                if (p.residual && row(u) < p.M && column(u) < p.N) residual[u % AHEAD] = load(of(row(u), p.residual, p.r_sb, p.r_sn), column(u));
+            };
+            if constexpr (!BARE) {
+                if (p.gate && one_sample) {
+#pragma unroll
+                    for (int c = 0; c < SIDE + FN % 2; ++c) {
+                        const int n = column(c < SIDE ? c : UNITS);
+                        if (n < p.N) gate[c] = load(p.gate + first_sample * p.g_sb, n);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) load_residual(u);
+            }
+#pragma unroll
+            for (int u = 0; u < ALL; ++u) {
+                const int i = u < UNITS ? 2 * (u % SIDE) : FN - 1, j = u < UNITS ? u / SIDE : 2 * (u - UNITS);
+                const f32x4 a = acc[i][j], b = u < UNITS ? acc[i + 1][j] : acc[i][j + 1];
+                float z[8];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[q]), __float_as_uint(b[q]), false, false);
+                    z[q] = __uint_as_float(both[0]);
+                    z[4 + q] = __uint_as_float(both[1]);
+                }
+                const int m = row(u), n = column(u);
+                bf16x8 out;
+                if constexpr (BARE) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) out[q] = (__bf16)z[q];
+                } else {
+                    bf16x8 by = gate[u < UNITS ? u % SIDE : SIDE];
+                    if (!SMOOTH && p.gate && !one_sample && m < p.M && n < p.N) by = load(of(m, p.gate, p.g_sb, 0), n);
+                    out = finished(p, z, by, residual[u % AHEAD]);
+                    if (u + AHEAD < ALL) load_residual(u + AHEAD);
+                }
+                if (u == ALL / 2 && more) load_bias();     // (half of the sums' registers are free)
+                if (m < p.M && n < p.N) {
+                    __bf16* y = (__bf16*)of(m, p.y, p.y_sb, p.y_sn);
+                    if constexpr (SMOOTH) *(bf16x8_anywhere*)(y + n) = out;
+                    else store_eight(y, n, p.N, out);
+                }
+            }
         };
-        if (p.gate && one_sample) {
-#pragma unroll
-            for (int c = 0; c < SIDE + FN % 2; ++c) {
-                const int n = column(c < SIDE ? c : UNITS);
-                if (n < p.N) gate[c] = eight_of(p.gate + first_sample * p.g_sb, n, p.N);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) load_residual(u);
-#pragma unroll
-        for (int u = 0; u < ALL; ++u) {
-            const int i = u < UNITS ? 2 * (u % SIDE) : FN - 1, j = u < UNITS ? u / SIDE : 2 * (u - UNITS);
-            const f32x4 a = acc[i][j], b = u < UNITS ? acc[i + 1][j] : acc[i][j + 1];
-            float z[8];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[q]), __float_as_uint(b[q]), false, false);
-                z[q] = __uint_as_float(both[0]);
-                z[4 + q] = __uint_as_float(both[1]);
-            }
-            const int m = row(u), n = column(u);
-            bf16x8 by = gate[u < UNITS ? u % SIDE : SIDE];
-            if (p.gate && !one_sample && m < p.M && n < p.N) by = eight_of(of(m, p.gate, p.g_sb, 0), n, p.N);
-            const bf16x8 out = finished(p, z, by, residual[u % AHEAD]);
-            if (u + AHEAD < ALL) load_residual(u + AHEAD);
-            if (u == ALL / 2 && more) load_bias();     // (half of the sums' registers are free)
-            if (m < p.M && n < p.N) store_eight((__bf16*)of(m, p.y, p.y_sb, p.y_sn), n, p.N, out);
-        }
+        if (!one_sample || (p.N % 8 != 0 && tile_right > p.N)) results(std::false_type(), std::false_type());
+        else if (p.activation == RAPID_ACT_NONE && !p.gate && !p.residual) results(std::true_type(), std::true_type());
+        else results(std::true_type(), std::false_type());
         }
         if (!more) break;
+        stored = true;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies, of nothing, write zeros: not into another workgroup's LDS
 }
