@@ -622,17 +622,17 @@ struct Plan {
 // What a product takes, in us.  Its items (tiles times pieces) go to 256 CUs with each slots of them at a time: full rounds, whose
 // steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full`; every round
 // has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.  Pieces are added up by a second kernel,
-// which costs `join` and `sum` for every million numbers that it reads.  Fitted to 800 products of 5 to 32768 rows, 16 to 9728
+// which costs `join` and `sum` for every million numbers that it reads.  Fitted to 800 products of 9 to 32768 rows, 16 to 9728
 // outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8 pieces, inputs changing
-// from call to call: the plan found by it takes 1.013 times what the best one does in the geometric mean (1.37 times at most).
+// from call to call: the plan found by it takes 1.014 times what the best one does in the geometric mean (1.27 times at most).
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;
 };
 constexpr TileCost COST[TILES] = {
-    {64, 64, 4, 0.352f, 0.887f, 2.38f, 0.51f, 2.21f, 1.36f, 2.46f}, {128, 128, 2, 0.439f, 1.119f, 3.97f, 0.63f, 1.92f, 1.23f, 1.94f},
-    {256, 160, 1, 0.660f, 1.115f, 5.84f, 0.75f, 1.36f, 0.f, 0.f},   {256, 192, 1, 0.796f, 1.378f, 5.96f, 0.80f, 1.56f, 0.f, 0.f},
-    {256, 256, 1, 0.994f, 1.765f, 7.21f, 0.84f, 1.59f, 0.f, 0.f}};
+    {64, 64, 4, 0.369f, 0.886f, 1.85f, 1.18f, 2.11f, 1.89f, 2.33f}, {128, 128, 2, 0.448f, 1.123f, 3.08f, 2.11f, 1.82f, 2.00f, 2.09f},
+    {256, 160, 1, 0.631f, 1.103f, 4.86f, 2.33f, 1.30f, 0.f, 0.f},   {256, 192, 1, 0.773f, 1.366f, 4.72f, 2.89f, 1.52f, 0.f, 0.f},
+    {256, 256, 1, 0.980f, 1.738f, 6.03f, 4.27f, 1.12f, 0.f, 0.f}};
 
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
