@@ -61,11 +61,12 @@ typedef enum {
  *             outputs and many inputs then take longer.  Contents on entry do not matter, nothing in it survives as state; one
  *             workspace must not serve two calls that can run concurrently.
  *   constraints  K a multiple of 8; x, w 16-byte aligned, their strides multiples of 8; y, residual, bias, gate 2-byte aligned;
- *             K <= w_stride <= 2^22; N <= 2^22; B*n < 2^31 - 256.  N, B and n may be anything (odd widths are stored element by
- *             element).  The rows of two consecutive samples of x (of 256, where n is small) lie within 2^30 elements.
+ *             K <= w_stride <= 2^22; N <= 2^22; B*n < 2^31 - 256.  N, B and n may be anything (what is left of a row behind its
+ *             last eight outputs is written element by element).  The rows of two consecutive samples of x (of 256, where n is small) lie within 2^30 elements.
  * y shares no byte with x, w, bias or gate, and none with residual but as above.
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE (sizes, strides); RAPID_ERR_UNSUPPORTED (K % 8, activation); RAPID_ERR_ALIGN;
- * RAPID_ERR_WORKSPACE (given, but too small or not aligned); RAPID_ERR_ALIAS (y starts where x or w does); RAPID_ERR_DEVICE.
+ * RAPID_ERR_WORKSPACE (given, but too small or not aligned); RAPID_ERR_ALIAS (y starts where x, w, bias or gate does, or where
+ * residual does and has other strides); RAPID_ERR_DEVICE.
  */
 RAPID_API int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const void* bias, const rapid_rows* y,
                            int activation, const void* gate, long long gate_stride, const rapid_rows* residual,
@@ -80,7 +81,8 @@ RAPID_API size_t rapid_linear_workspace_bytes(long long M, int N, int K);
  *   x, y     device, bf16, rows [B, n, C]; y may be x, element for element, and else shares no byte with an input
  *   scale, shift  device, bf16, row b (of C elements) at ptr + b*stride; both or neither (NULL: the norm alone)
  *   eps      >= 0
- *   constraints  C a multiple of 8, at most 16384; pointers 16-byte aligned, strides multiples of 8; B*n < 2^31 - 256
+ *   constraints  C a multiple of 8, at most 16384; pointers 16-byte aligned, strides multiples of 8; B*n at most 2^26 - 4
+ *                (above C = 2048: 2^25 - 4, above 4096: 2^24 - 4, above 8192: 2^23 - 4)
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE; RAPID_ERR_UNSUPPORTED (C); RAPID_ERR_ALIGN; RAPID_ERR_ALIAS (y starts where x does
  * and has other strides, or where scale or shift does); RAPID_ERR_DEVICE.
  */
@@ -152,8 +154,8 @@ typedef enum {
  *            are handled by other rules, or a learned one.
  *   rot      multiple of 16, at most D
  *   constraints  D 64 or 128; 16-byte aligned pointers (weights too); strides multiples of 8 elements, 0 <= stride_b, stride_h,
- *            stride_n <= 2^40 (those of dimensions of size 1 not looked at); out strides other than 0; B*H <= 524287, N <= 2^22;
- *            table_stride_b a multiple of 4
+ *            stride_n <= 2^40 (those of dimensions of size 1 not looked at), out strides at least D; B*H <= 524287, N <= 2^22,
+ *            B*N*ceil(H/2)*D <= 2^35 - 2048; table_stride_b a multiple of 4
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE; RAPID_ERR_UNSUPPORTED (D, rot, layout); RAPID_ERR_ALIGN; RAPID_ERR_ALIAS (q_out
  * starts where k_out or k does, k_out where q does, or an output where its input does with other strides); RAPID_ERR_DEVICE.
  */

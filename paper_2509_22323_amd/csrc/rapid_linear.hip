@@ -711,7 +711,8 @@ int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const v
     if (!aligned(y->ptr, 2) || !aligned(bias, 2) || !aligned(gate, 2) || (residual && !aligned(residual->ptr, 2))) return RAPID_ERR_ALIGN;
     // rows of one tile are addressed from its first sample by 32 bits
     if (B > 1 && (255 / n + 1) * p.x_sb + (long long)(n - 1) * p.x_sn + K > (1LL << 30)) return RAPID_ERR_SHAPE;
-    if (y->ptr == x->ptr || y->ptr == w) return RAPID_ERR_ALIAS;
+    if (y->ptr == x->ptr || y->ptr == w || y->ptr == bias || y->ptr == gate) return RAPID_ERR_ALIAS;
+    if (residual && y->ptr == residual->ptr && (p.y_sb != p.r_sb || p.y_sn != p.r_sn)) return RAPID_ERR_ALIAS;
     const size_t need = workspace ? rapid_linear_workspace_bytes(M, N, K) : 0;
     if (workspace && (workspace_bytes < need || !aligned(workspace, 16))) return RAPID_ERR_WORKSPACE;
     p.x = (const __bf16*)x->ptr;

@@ -2,6 +2,7 @@
 weights of its own, joined for attention alone; every projection under the conditioning of the time step).
 
 Weights are the caller's (there are none here); buffers are made once, a run allocates nothing and can be captured into a graph.
+Runs of one layer, graphs of them included, share its buffers: they follow each other, on the stream that it was made on or behind it.
 """
 from __future__ import annotations
 
@@ -19,7 +20,7 @@ WEIGHTS = ("mod_w", "mod_b",           # [6C, C]: shift, scale, gate of the atte
 class JointLayer:
     """weights: (of the image stream, of the text stream), each a dict of CUDA bf16 tensors named as in WEIGHTS (biases and norms
     may be None).  positions (CUDA int32 [image + text, axes]) and axes (RopeAxis each): the rotation of queries and keys; None =
-    none.  image is a multiple of 128."""
+    none.  image is a multiple of 128, F of 8."""
 
     def __init__(self, weights, B, H, D, image, text, positions=None, axes=None, layout="interleaved", eps=1e-6):
         import torch

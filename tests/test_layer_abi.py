@@ -151,3 +151,37 @@ def test_python_forms_take_tensors_of_the_gpu_alone():
     for call in (lambda: ra.rapid_rope([], x), lambda: ra.rapid_rope([(q, q, q, q)], x, "other"), lambda: ra.RopeAxis(64, scaling="other")):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(bias=3 * A), dict(gate=3 * A), dict(res=(3 * A, 0, 40)), dict(B=2, x=(A, 256, 64), y=(3 * A, 128, 32), res=(3 * A, 256, 32)),
+    dict(B=2, x=(A, 256, 64), y=(3 * A, 128, 32), res=(3 * A, 0, 32)), dict(res=(3 * A, 0, 0))], ids=str)
+def test_linear_outputs_that_begin_where_something_added_does(kw):
+    assert linear(**kw) == ALIAS
+
+
+@pytest.mark.parametrize("C,rows", [(8, 1 << 26), (2048, 1 << 26), (2056, 1 << 25), (8192, 1 << 24), (16384, 1 << 23)])
+def test_rows_that_a_launch_does_not_hold(C, rows):
+    for n in (rows, (1 << 31) - 257):
+        assert modulate(x=(A, 0, C), y=(3 * A, 0, C), n=n, C=C) == SHAPE
+
+
+def test_heads_that_a_launch_does_not_hold():
+    assert qk(B=1 << 8, H=1 << 9, D=128, segs=({"n": 1 << 22, "out_b": 1 << 40, "out_n": 128, "out_h": 1 << 30, "in_n": 128},), rot=64) == SHAPE
+
+
+@pytest.mark.parametrize("axis", [(64, 1e-6, "none"), (64, 1e4, "linear", 1e-6), (64, 1e-12, "ntk", 2.0)], ids=str)
+def test_turns_that_cannot_be_reduced(axis):
+    assert table(axes=(axis,)) == UNSUPPORTED
+
+
+@pytest.mark.skipif(binding._load_native().__class__ is binding._NoNative, reason="the native calls are not built for this torch")
+def test_native_forms_leave_other_tensors_to_the_python_form():
+    x, q = torch.zeros((1, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 2, 4, 64), dtype=torch.bfloat16)
+    positions, turns = torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, 32, 2)
+    native = binding._load_native()
+    assert native.linear(x, x[0], x, None, "none", None, None, None) is None
+    assert native.modulate(x, x, None, None, 1e-6) is None
+    assert native.table(positions, [ra.RopeAxis(64)], turns, 1.0) is None
+    assert native.qk_norm_rope([(q, q, q, q)], None, turns, "interleaved", 1e-6) is None
+    assert native.rope([(q, q, q, q)], None, turns, "half") is None
