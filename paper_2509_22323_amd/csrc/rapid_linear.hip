@@ -1,6 +1,11 @@
 // Linear layers of an MM-DiT layer for MI355X (gfx950): y = residual + gate * act(x w^T + bias).
 // C ABI: include/rapid_layer.h.
+//
+// A handful of rows: linear_dot_kernel (bound by the bytes of w).  Everything else: linear_wide_kernel, tiles of matrix instructions,
+// and where a product has few tiles and many inputs, linear_join_kernel behind it, which adds up pieces along K.  by_dots and
+// plan_for at the end of the file choose.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -112,8 +117,17 @@ __device__ __forceinline__ bf16x8 finished(const LinearParams& p, float (&z)[8],
 }
 
 // ---------------------------------------------------------------------------
-// Large products: 256 x 32*FN outputs per workgroup of 8 wavefronts (4 along the rows of x, 2 along those of w; a wavefront has
-// 64 x 16*FN), 64 inputs per step.
+// Tiles: 64*WR x 32*FN outputs per workgroup of 2*WR wavefronts (WR along the rows of x, two along those of w; a wavefront has
+// 64 x 16*FN), 64 inputs per step.  The operands change places, A = rows of w and B = rows of x, so that a lane ends with four outputs of a
+// row side by side.  Copies go from memory into LDS past the registers, two or three steps ahead, one barrier a step; workgroups
+// stay and go on to their next item, whose first steps are on their way before the results of the last one are written.
+//
+// Bound by the matrix pipe and the clock it leaves: 8192 rows, 9728 -> 2432 (388 GFLOP, tile 256 x 160) takes 291 us = 1.33 PFLOP/s, the
+// pipe busy 72 % of the cycles; the same loop without copies 264, without reads of LDS 250, without either 234, without the barrier 285.
+// 8192 rows, 1536 -> 4608 (116 GFLOP, 256 x 192): 99 us, of which the ends of tiles are a sixth.  Measured and not taken: other
+// orders of tiles (GROUP 2, 6, 8, 16), weights past the caches, touching the next steps in the L2 first, 128 x 64 outputs a wavefront
+// with four wavefronts, all copies in a step's first half, priorities of waves, five steps in LDS for the small tiles: none faster over
+// products of 64 to 8192 rows, most 1 to 20 % slower.
 // ---------------------------------------------------------------------------
 constexpr int STEP = 64;                               // inputs per step: 128 bytes of a row
 constexpr int ROW = STEP * 2;
@@ -613,26 +627,27 @@ int launch_wide(const LinearParams& p, void* stream)
 // ---------------------------------------------------------------------------
 // Which tile, and how many pieces along K
 // ---------------------------------------------------------------------------
-enum Tile { T64x64, T128x128, T256x160, T256x192, T256x256, TILES };
+enum Tile { T64x64, T128x128, T256x128, T256x160, T256x192, T256x256, TILES };
 struct Plan {
     Tile tile;
     int pieces;
 };
 
 // What a product takes, in us.  Its items (tiles times pieces) go to 256 CUs with each slots of them at a time: full rounds, whose
-// steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full`; every round
-// has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.  Pieces are added up by a second kernel,
-// which costs `join` and `sum` for every million numbers that it reads.  Fitted to 800 products of 9 to 32768 rows, 16 to 9728
-// outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8 pieces, inputs changing
-// from call to call: the plan found by it takes 1.014 times what the best one does in the geometric mean (1.27 times at most).
+// steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full` (the fullest CU
+// counts more than the mean); every round has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.
+// Pieces are added up by a second kernel, which costs `join` and `sum` for every million numbers that it reads.  Fitted to 1050
+// products of 9 to 32768 rows, 16 to 9728 outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8
+// pieces, inputs changing from call to call: the plan found by it takes 1.009 times what the best one does in the geometric mean
+// (1.33 times at most).
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;
 };
 constexpr TileCost COST[TILES] = {
-    {64, 64, 4, 0.369f, 0.886f, 1.85f, 1.18f, 2.11f, 1.89f, 2.33f}, {128, 128, 2, 0.448f, 1.123f, 3.08f, 2.11f, 1.82f, 2.00f, 2.09f},
-    {256, 160, 1, 0.631f, 1.103f, 4.86f, 2.33f, 1.30f, 0.f, 0.f},   {256, 192, 1, 0.773f, 1.366f, 4.72f, 2.89f, 1.52f, 0.f, 0.f},
-    {256, 256, 1, 0.980f, 1.738f, 6.03f, 4.27f, 1.12f, 0.f, 0.f}};
+    {64, 64, 4, 0.396f, 0.789f, 1.62f, 1.18f, 2.42f, 2.13f, 1.85f}, {128, 128, 2, 0.508f, 0.939f, 3.37f, 2.27f, 1.60f, 2.95f, 1.23f},
+    {256, 128, 1, 0.540f, 0.856f, 3.64f, 2.38f, 2.38f, 0.f, 0.f},   {256, 160, 1, 0.649f, 0.992f, 5.45f, 2.48f, 1.27f, 0.f, 0.f},
+    {256, 192, 1, 0.805f, 1.236f, 5.12f, 3.36f, 1.56f, 0.f, 0.f},   {256, 256, 1, 0.996f, 1.555f, 6.51f, 4.70f, 1.54f, 0.f, 0.f}};
 
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
@@ -642,7 +657,7 @@ float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
     const float ends = N % 8 != 0 && pieces == 1 ? c.ends + c.odd : c.ends;
     float t = c.call + (float)(items / slots) * (steps * c.full + ends);
     if (items % slots != 0) {
-        const float crowd = c.slots == 1 ? load : load > 1.f ? (load - 1.f) / (c.slots - 1) : 0.f;
+        const float crowd = c.slots == 1 ? load : load > 1.f ? (0.3f * load + 0.7f * ceilf(load) - 1.f) / (c.slots - 1) : 0.f;
         t += steps * (c.alone + (c.full - c.alone) * crowd) + ends;
     }
     return pieces > 1 ? t + c.join + c.sum * 1e-6f * (float)M * (float)N * pieces : t;
@@ -742,6 +757,7 @@ int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const v
     switch (plan.tile) {
     case T64x64: return launch_wide<1, 2, false>(p, stream);
     case T128x128: return launch_wide<2, 4, false>(p, stream);
+    case T256x128: return launch_wide<4, 4, false>(p, stream);
     case T256x160: return launch_wide<4, 5, false>(p, stream);
     case T256x192: return launch_wide<4, 6, false>(p, stream);
     default: return launch_wide<4, 8, false>(p, stream);

@@ -222,3 +222,10 @@ def test_without_a_workspace():
         with pytest.raises(ra.RapidAttnError) as e:
             ra.rapid_linear(x, w, out, workspace=small)
         assert e.value.status == ra.STATUS["RAPID_ERR_WORKSPACE"]
+
+
+@pytest.mark.parametrize("size", [(2, 333, 2432, 9728), (1, 666, 2440, 9721), (2, 2048, 6144, 1536), (3, 683, 4000, 4090)], ids=str)
+def test_middling_products(size):
+    """Fewer large tiles than the card has CUs, or not many more: 256 x 128 and 256 x 160."""
+    test_large(size, True)
+    test_large(size, False)
