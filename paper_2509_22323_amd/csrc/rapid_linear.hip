@@ -53,6 +53,7 @@ struct LinearParams {
     int activation;
     int pieces, pitch;       // a product in pieces along K: how many, and floats from row to row of their sums
     float* partial;          // [pieces, M, pitch]
+    bool even;               // 16 bytes an access in the epilogue, see even_rows
 };
 
 // The sample and row of row m.
@@ -72,27 +73,89 @@ __device__ __forceinline__ float activated(float z, int activation)
     return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(e));
 }
 
-// What the epilogue adds and multiplies, and writes, eight outputs at a time: rows of odd widths start anywhere, so these accesses
-// may be aligned to two bytes only (the memory pipeline takes them).
+// What the epilogue adds and multiplies, and writes, eight outputs at a time.  Rows of odd widths start anywhere; an access of 16 bytes is
+// as fast at any multiple of four, but takes twice as long and more at odd numbers of elements (75 MB written by 8192 rows of 4608: 32 us
+// and 55), where it is made in pieces instead: the first element, three pairs and the last one (43 us).
 typedef bf16x8 bf16x8_anywhere __attribute__((aligned(2)));
 typedef bf16x4 bf16x4_anywhere __attribute__((aligned(2)));
+typedef unsigned u32_alias __attribute__((may_alias));
+typedef unsigned short u16_alias __attribute__((may_alias));
 
-// Outputs j .. j + 7 of a row, or as many as there are
-__device__ __forceinline__ bf16x8 eight_of(const __bf16* at, int j, int N)
+__device__ __forceinline__ bool odd(const __bf16* at, bool even) { return !even && ((uintptr_t)at & 2) != 0; }
+
+// Eight elements as they were loaded: the four pairs, or the three inner ones, the first and the last element.
+struct Loaded {
+    unsigned d[5];
+};
+__device__ __forceinline__ Loaded loaded(const __bf16* at, bool even)
 {
-    if (j + 8 <= N) return *(const bf16x8_anywhere*)(at + j);
-    bf16x8 v = {};
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (j + i < N) v[i] = at[j + i];
+    Loaded v;
+    if (odd(at, even)) {
+        const u32_alias* inner = (const u32_alias*)(at + 1);
+        v.d[0] = inner[0];
+        v.d[1] = inner[1];
+        v.d[2] = inner[2];
+        v.d[3] = *(const u16_alias*)at;
+        v.d[4] = *(const u16_alias*)(at + 7);
+    } else {
+        const u32x4 pairs = __builtin_bit_cast(u32x4, (bf16x8)*(const bf16x8_anywhere*)at);
+        v.d[0] = pairs[0];
+        v.d[1] = pairs[1];
+        v.d[2] = pairs[2];
+        v.d[3] = pairs[3];
+        v.d[4] = 0;
+    }
     return v;
 }
-__device__ __forceinline__ void store_eight(__bf16* at, int j, int N, bf16x8 v)
+__device__ __forceinline__ bf16x8 eight(const Loaded& v, bool odd)
 {
-    if (j + 8 <= N) { *(bf16x8_anywhere*)(at + j) = v; return; }
+    const unsigned d0 = odd ? v.d[0] << 16 | v.d[3] : v.d[0], d1 = odd ? __builtin_amdgcn_alignbit(v.d[1], v.d[0], 16) : v.d[1];
+    const unsigned d2 = odd ? __builtin_amdgcn_alignbit(v.d[2], v.d[1], 16) : v.d[2], d3 = odd ? v.d[4] << 16 | v.d[2] >> 16 : v.d[3];
+    return __builtin_bit_cast(bf16x8, (u32x4){d0, d1, d2, d3});
+}
+__device__ __forceinline__ void store(__bf16* at, bf16x8 v, bool even)
+{
+    if (odd(at, even)) {
+        const u32x4 d = __builtin_bit_cast(u32x4, v);
+        const unsigned d0 = d[0], d1 = d[1], d2 = d[2], d3 = d[3];
+        u32_alias* inner = (u32_alias*)(at + 1);
+        inner[0] = __builtin_amdgcn_alignbit(d1, d0, 16);
+        inner[1] = __builtin_amdgcn_alignbit(d2, d1, 16);
+        inner[2] = __builtin_amdgcn_alignbit(d3, d2, 16);
+        *(u16_alias*)at = (unsigned short)d0;
+        *(u16_alias*)(at + 7) = (unsigned short)(d3 >> 16);
+    } else {
+        *(bf16x8_anywhere*)at = v;
+    }
+}
+
+// Outputs j .. j + 7 of a row, or as many as there are (what the others hold is not used)
+__device__ __forceinline__ Loaded loaded(const __bf16* at, int j, int N, bool even)
+{
+    if (j + 8 <= N) return loaded(at + j, even);
+    unsigned e[8] = {};
 #pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (j + i < N) at[j + i] = v[i];
+    for (int i = 0; i < 7; ++i) e[i] = ((const u16_alias*)at)[min(j + i, N - 1)];
+    Loaded v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.d[i] = e[2 * i] | e[2 * i + 1] << 16;
+    v.d[4] = 0;
+    return v;
+}
+__device__ __forceinline__ bf16x8 eight(const Loaded& v, const __bf16* at, int j, int N, bool even)
+{
+    return eight(v, odd(at + j, even) && j + 8 <= N);
+}
+__device__ __forceinline__ bf16x8 eight_of(const __bf16* at, int j, int N, bool even) { return eight(loaded(at, j, N, even), at, j, N, even); }
+__device__ __forceinline__ void store_eight(__bf16* at, int j, int N, bf16x8 v, bool even)
+{
+    if (j + 8 <= N) { store(at + j, v, even); return; }
+    const u32x4 d = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+        const unsigned two = d[i / 2];
+        if (j + i < N) ((u16_alias*)at)[j + i] = (unsigned short)(i % 2 ? two >> 16 : two);
+    }
 }
 
 // residual + gate * act(sum), everything in fp32, rounded once.  (What is not there is skipped by scalar branches.)
@@ -185,6 +248,13 @@ __device__ __forceinline__ void tile_of(int t, int mt, int nt, int& m, int& n)
     m = run * GROUP + in - n * rows;
 }
 
+// A pointer into the GPU's memory (and not to LDS, which nothing says of one that is read from an argument block)
+template <typename T>
+__device__ __forceinline__ T* in_memory(T* p)
+{
+    return (T*)(__attribute__((address_space(1))) T*)(uintptr_t)p;
+}
+
 template <int WR, int FN, bool SPLIT>
 __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p, int items)
 {
@@ -230,7 +300,24 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         m0 = __builtin_amdgcn_readfirstlane(mi) * TM;
         j0 = __builtin_amdgcn_readfirstlane(ni) * TN;
     };
-    // (The lane's number, such that nothing made from it is kept in registers over the loops.)
+    // The arguments read again, and the lane's number, such that nothing made from them is kept in registers over the loops (scalar
+    // ones that do not fit go to lanes of vector registers, and back in every step).
+    auto arguments = [] {
+        auto at = __builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(at));
+        struct Words {
+            unsigned long long word[sizeof(LinearParams) / 8];
+        } words;
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(LinearParams) / 8; ++i) words.word[i] = ((const __attribute__((address_space(4))) unsigned long long*)at)[i];
+        LinearParams p = __builtin_bit_cast(LinearParams, words);
+        p.bias = in_memory(p.bias);
+        p.gate = in_memory(p.gate);
+        p.residual = in_memory(p.residual);
+        p.y = in_memory(p.y);
+        p.partial = in_memory(p.partial);
+        return p;
+    };
     auto lane_here = [&] {
         int l = lane;
         asm volatile("" : "+v"(l));
@@ -242,6 +329,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     auto sources_x = [&] {
         int r0;
         const int lane = lane_here();
+        const LinearParams p = arguments();
         sample_of(p, m0, b0, r0);
         b0 = __builtin_amdgcn_readfirstlane(b0);
         r0 = __builtin_amdgcn_readfirstlane(r0);
@@ -256,6 +344,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     };
     auto sources_w = [&] {
         const int lane = lane_here();
+        const LinearParams p = arguments();
         wbuffer = buffer_at(p.w + (long long)j0 * p.w_sn);
         wk = (first + turn) * ROW;
 #pragma unroll
@@ -318,6 +407,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
     bf16x4 bias[FN] = {};
     auto load_bias = [&] {
         const int n = j0 + wn * 16 * FN + 4 * (lane_here() >> 4);
+        const LinearParams p = arguments();
         if (SPLIT || p.bias == nullptr) return;
 #pragma unroll
         for (int i = 0; i < FN; ++i) {
@@ -359,7 +449,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
             for (int j = 0; j < FM; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) acc[i][j][q] = (float)bias[i][q];
-        const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_end = min(m0 + TM, p.M), tile_right = j0 + TN;
+        const int mw = m0 + wm * 16 * FM, nw = j0 + wn * 16 * FN, first_sample = b0, own_piece = piece, tile_first = m0, tile_right = j0 + TN;
         const bool more = id + (int)gridDim.x < items;
         const int length = steps;
         // A step's buffer is free once its second half is in registers; behind the last steps follow the first ones of this
@@ -405,6 +495,7 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         }
 
         const int lane = lane_here();
+        const LinearParams p = arguments();
         if constexpr (SPLIT) {                         // this piece's sums, as they are
             const int n = nw + 4 * (lane >> 4);
 #pragma unroll
@@ -419,37 +510,52 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
         // Pairs of fragments trade rows of lanes, so that a lane has eight consecutive outputs of a row: of (a, b) the lanes of
         // rows 0, 2 get a's 0..7 and 8..15, those of rows 1, 3 b's.  Fragments side by side; of an odd number the last ones in
         // pairs below each other.
-        const bool one_sample = one || tile_end <= (first_sample + 1) * p.n;
+        const bool one_sample = one || min(tile_first + TM, p.M) <= (first_sample + 1) * p.n;
         const int g = lane >> 4;
         constexpr int SIDE = FN / 2, UNITS = FM * SIDE, ALL = UNITS + (FN % 2) * FM / 2;
         auto row = [&](int u) { return mw + 16 * (u < UNITS ? u / SIDE : 2 * (u - UNITS) + (g & 1)) + (lane & 15); };
         auto column = [&](int u) { return nw + (u < UNITS ? 32 * (u % SIDE) + (g & 1) * 16 : 16 * (FN - 1)) + (g >> 1) * 8; };
-        // Smooth: one sample, and eight outputs or none wherever a lane writes.  Bare: neither activation, gate nor residual.  Most
-        // tiles need the smooth forms alone, which are short (one form for all cases, 7000 instructions long: 7 us a tile of
-        // 256 x 192).
-        auto results = [&](auto smooth, auto bare) {
-            constexpr bool SMOOTH = smooth.value, BARE = bare.value;
+        // Whole: eight outputs or none wherever a lane writes.  Even: 16 bytes an access.
+        // Single: one sample.  Bare: neither activation, gate nor residual.  Most tiles need the first two forms alone, which are
+        // short (one form for all cases, 7000 instructions long: 7 us a tile of 256 x 192).
+        auto results = [&](auto whole, auto even, auto single, auto bare) {
+            constexpr bool WHOLE = whole.value, EVEN = even.value, SINGLE = single.value, BARE = bare.value;
             auto of = [&](int m, const __bf16* t, long long sb, int sn) {   // row m of a tensor
                 int b = first_sample, r = m - first_sample * p.n;
-                if (!SMOOTH && !one_sample) sample_of(p, m, b, r);
+                if (!SINGLE && !one_sample) sample_of(p, m, b, r);
                 return t + b * sb + (long long)r * sn;
             };
-            auto load = [&](const __bf16* at, int n) { return SMOOTH ? (bf16x8)*(const bf16x8_anywhere*)(at + n) : eight_of(at, n, p.N); };
-            constexpr int AHEAD = ALL < 6 ? ALL : 6;       // residuals on their way
-            bf16x8 gate[SIDE + 1] = {}, residual[AHEAD] = {};
-            auto load_residual = [&](int u) {
-                if (p.residual && row(u) < p.M && column(u) < p.N) residual[u % AHEAD] = load(of(row(u), p.residual, p.r_sb, p.r_sn), column(u));
+            typedef std::conditional_t<EVEN, bf16x8, Loaded> Eight;
+            auto load = [&](const __bf16* at, int n) {
+                if constexpr (EVEN) return (bf16x8)*(const bf16x8_anywhere*)(at + n);
+                else if constexpr (WHOLE) return loaded(at + n, false);
+                else return loaded(at, n, p.N, p.even);
+            };
+            auto value = [&](const Eight& v, const __bf16* at, int n) {
+                if constexpr (EVEN) return v;
+                else if constexpr (WHOLE) return eight(v, odd(at, false));
+                else return eight(v, at, n, p.N, p.even);
+            };
+            // residuals on their way, and gates where a tile has several (as many as there are registers for)
+            constexpr int MOST_AHEAD = EVEN ? FN == 8 ? 4 : 6 : FN == 8 ? 1 : 3, AHEAD = ALL < MOST_AHEAD ? ALL : MOST_AHEAD;
+            bf16x8 gate[SIDE + 1] = {};
+            Eight residuals[AHEAD] = {}, gates[SINGLE ? 1 : AHEAD] = {};
+            auto load_ahead = [&](int u) {
+                const int m = row(u), n = column(u);
+                if (m >= p.M || n >= p.N) return;
+                if (p.residual) residuals[u % AHEAD] = load(of(m, p.residual, p.r_sb, p.r_sn), n);
+                if (!SINGLE && p.gate && !one_sample) gates[u % AHEAD] = load(of(m, p.gate, p.g_sb, 0), n);
             };
             if constexpr (!BARE) {
                 if (p.gate && one_sample) {
 #pragma unroll
                     for (int c = 0; c < SIDE + FN % 2; ++c) {
                         const int n = column(c < SIDE ? c : UNITS);
-                        if (n < p.N) gate[c] = load(p.gate + first_sample * p.g_sb, n);
+                        if (n < p.N) gate[c] = eight_of(p.gate + first_sample * p.g_sb, n, p.N, p.even);
                     }
                 }
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) load_residual(u);
+                for (int u = 0; u < AHEAD; ++u) load_ahead(u);
             }
 #pragma unroll
             for (int u = 0; u < ALL; ++u) {
@@ -469,21 +575,30 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p
                     for (int q = 0; q < 8; ++q) out[q] = (__bf16)z[q];
                 } else {
                     bf16x8 by = gate[u < UNITS ? u % SIDE : SIDE];
-                    if (!SMOOTH && p.gate && !one_sample && m < p.M && n < p.N) by = load(of(m, p.gate, p.g_sb, 0), n);
-                    out = finished(p, z, by, residual[u % AHEAD]);
-                    if (u + AHEAD < ALL) load_residual(u + AHEAD);
+                    bf16x8 residual = {};
+                    if (p.residual) residual = value(residuals[u % AHEAD], of(m, p.residual, p.r_sb, p.r_sn), n);
+                    if (!SINGLE && p.gate && !one_sample) by = value(gates[u % AHEAD], of(m, p.gate, p.g_sb, 0), n);
+                    out = finished(p, z, by, residual);
+                    if (u + AHEAD < ALL) load_ahead(u + AHEAD);
                 }
                 if (u == ALL / 2 && more) load_bias();     // (half of the sums' registers are free)
                 if (m < p.M && n < p.N) {
                     __bf16* y = (__bf16*)of(m, p.y, p.y_sb, p.y_sn);
-                    if constexpr (SMOOTH) *(bf16x8_anywhere*)(y + n) = out;
-                    else store_eight(y, n, p.N, out);
+                    if constexpr (EVEN) *(bf16x8_anywhere*)(y + n) = out;
+                    else if constexpr (WHOLE) store(y + n, out, false);
+                    else store_eight(y, n, p.N, out, p.even);
                 }
             }
         };
-        if (!one_sample || (p.N % 8 != 0 && tile_right > p.N)) results(std::false_type(), std::false_type());
-        else if (p.activation == RAPID_ACT_NONE && !p.gate && !p.residual) results(std::true_type(), std::true_type());
-        else results(std::true_type(), std::false_type());
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
+        const bool cut = p.N % 8 != 0 && tile_right > p.N, bare_call = p.activation == RAPID_ACT_NONE && !p.gate && !p.residual;
+        if (__builtin_expect(p.even && one_sample && !cut, 1)) {
+            if (bare_call) results(yes, yes, yes, yes);
+            else results(yes, yes, yes, no);
+        } else if (cut || !(one_sample || p.even)) results(no, no, no, no);
+        else if (one_sample) results(yes, no, yes, no);
+        else results(yes, yes, no, no);
         }
         if (!more) break;
         stored = true;
@@ -500,9 +615,9 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
     int b, r;
     sample_of(p, (int)m, b, r);
     bf16x8 bias = {}, gate = {}, residual = {};
-    if (p.bias) bias = eight_of(p.bias, n, p.N);
-    if (p.gate) gate = eight_of(p.gate + b * p.g_sb, n, p.N);
-    if (p.residual) residual = eight_of(p.residual + b * p.r_sb + (long long)r * p.r_sn, n, p.N);
+    if (p.bias) bias = eight_of(p.bias, n, p.N, p.even);
+    if (p.gate) gate = eight_of(p.gate + b * p.g_sb, n, p.N, p.even);
+    if (p.residual) residual = eight_of(p.residual + b * p.r_sb + (long long)r * p.r_sn, n, p.N, p.even);
     float z[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i] = (float)bias[i];
@@ -519,7 +634,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
         if (s < p.pieces)
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] += part[s][i / 4][i % 4];
-    store_eight(p.y + b * p.y_sb + (long long)r * p.y_sn, n, p.N, finished(p, z, gate, residual));
+    store_eight(p.y + b * p.y_sb + (long long)r * p.y_sn, n, p.N, finished(p, z, gate, residual), p.even);
 }
 
 // ---------------------------------------------------------------------------
@@ -600,6 +715,14 @@ __global__ __launch_bounds__(DOT_WAVES * 64) void linear_dot_kernel(LinearParams
 // 6144 -> 1536, but 20.5 / 16.7 at 2432 -> 14592.
 bool by_dots(long long M, int N, int K) { return M <= 4 || (M <= 8 && (long long)N * K <= 1 << 24); }
 
+// Rows of y, residual and gate that start at multiples of four bytes, or results too small for it to matter: 8192 rows, 1536 -> 4607 with
+// gate and residual 148 us, and 129 in pieces; 2388 rows, 392 -> 2919 20.1 and 18.5; but 2009 rows, 280 -> 143 7.6 and 8.0.
+bool even_rows(const LinearParams& p)
+{
+    const uintptr_t starts = (uintptr_t)p.y | (uintptr_t)p.residual | (uintptr_t)p.gate | 2 * (uintptr_t)(p.y_sb | p.y_sn | p.r_sb | p.r_sn | p.g_sb);
+    return starts % 4 == 0 || (long long)p.M * p.N < 1 << 21;
+}
+
 template <int MAX_M>
 int launch_dot(const LinearParams& p, void* stream)
 {
@@ -635,19 +758,19 @@ struct Plan {
 
 // What a product takes, in us.  Its items (tiles times pieces) go to 256 CUs with each slots of them at a time: full rounds, whose
 // steps of 64 inputs take `full` each, and a last one whose steps take from `alone` (an item to a CU or less) to `full` (the fullest CU
-// counts more than the mean); every round has `ends` (`odd` more where output rows are not aligned to 16 bytes), every call `call`.
+// counts more than the mean); every round has `ends` (`odd` more where the width is no multiple of eight), every call `call`.
 // Pieces are added up by a second kernel, which costs `join` and `sum` for every million numbers that it reads.  Fitted to 1050
 // products of 9 to 32768 rows, 16 to 9728 outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8
-// pieces, inputs changing from call to call: the plan found by it takes 1.009 times what the best one does in the geometric mean
+// pieces, inputs changing from call to call: the plan found by it takes 1.010 times what the best one does in the geometric mean
 // (1.33 times at most).
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;
 };
 constexpr TileCost COST[TILES] = {
-    {64, 64, 4, 0.396f, 0.789f, 1.62f, 1.18f, 2.42f, 2.13f, 1.85f}, {128, 128, 2, 0.508f, 0.939f, 3.37f, 2.27f, 1.60f, 2.95f, 1.23f},
-    {256, 128, 1, 0.540f, 0.856f, 3.64f, 2.38f, 2.38f, 0.f, 0.f},   {256, 160, 1, 0.649f, 0.992f, 5.45f, 2.48f, 1.27f, 0.f, 0.f},
-    {256, 192, 1, 0.805f, 1.236f, 5.12f, 3.36f, 1.56f, 0.f, 0.f},   {256, 256, 1, 0.996f, 1.555f, 6.51f, 4.70f, 1.54f, 0.f, 0.f}};
+    {64, 64, 4, 0.397f, 0.787f, 1.62f, 1.28f, 2.40f, 2.16f, 1.85f}, {128, 128, 2, 0.507f, 0.936f, 3.39f, 2.15f, 1.79f, 2.72f, 1.24f},
+    {256, 128, 1, 0.541f, 0.845f, 3.72f, 2.20f, 2.59f, 0.f, 0.f},   {256, 160, 1, 0.647f, 0.987f, 5.59f, 2.23f, 1.28f, 0.f, 0.f},
+    {256, 192, 1, 0.792f, 1.212f, 5.21f, 2.97f, 1.88f, 0.f, 0.f},   {256, 256, 1, 0.996f, 1.537f, 6.63f, 3.56f, 1.80f, 0.f, 0.f}};
 
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
@@ -753,6 +876,7 @@ int rapid_linear(const rapid_rows* x, const void* w, long long w_stride, const v
     p.pieces = plan.pieces;
     p.pitch = (N + 7) / 8 * 8;
     p.partial = (float*)workspace;
+    p.even = even_rows(p);
     if (plan.pieces > 1) return plan.tile == T64x64 ? launch_wide<1, 2, true>(p, stream) : launch_wide<2, 4, true>(p, stream);
     switch (plan.tile) {
     case T64x64: return launch_wide<1, 2, false>(p, stream);
