@@ -178,3 +178,49 @@ def test_driver_runs_layers():
     np.testing.assert_array_equal(bits(out), co.cache_reuse(bits(x), step))
     with pytest.raises(ValueError):
         run_action_trace([(1, 0)], None, None, None, None, 1, 128, None, None, x, delta, out, layer=layer, conditioning=cond)
+
+
+def test_two_layers_at_once():
+    """Layers with buffers of their own on two streams, their calls interleaved: the bits of one after the other."""
+    pairs = [make(seed=s) for s in (11, 12)]
+    starts = [h.clone() for _, h, _ in pairs]
+    for layer, hidden, cond in pairs:
+        layer.run(*halves(layer, hidden), cond, 1)
+    want = [h.clone() for _, h, _ in pairs]
+    streams = [torch.cuda.Stream() for _ in pairs]
+    for _ in range(3):
+        for (_, hidden, _), start in zip(pairs, starts):
+            hidden.copy_(start)
+        torch.cuda.synchronize()
+        for stream, (layer, hidden, cond) in zip(streams, pairs):
+            with torch.cuda.stream(stream):
+                layer.run(*halves(layer, hidden), cond, 1)
+        torch.cuda.synchronize()
+        for (_, hidden, _), w in zip(pairs, want):
+            assert torch.equal(hidden, w)
+
+
+def test_products_on_two_streams_take_workspaces_of_their_own():
+    x, w = normal((2, 150, 4096), 1), normal((320, 4096), 2, 1 / 64)
+    assert ra.rapid_linear_workspace_bytes(300, 320, 4096) > 0
+    want = ra.rapid_linear(x, w, torch.empty((2, 150, 320), dtype=x.dtype, device="cuda"))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for i in range(8):
+        with torch.cuda.stream(streams[i % 2]):
+            outs.append(ra.rapid_linear(x, w, torch.empty_like(want)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_padding_that_is_not_a_number():
+    """Text rows behind a sample's length that hold no numbers: nothing of them reaches the rows before."""
+    layer, hidden, cond = make(text=100, seed=5)
+    lens = torch.tensor([256 + 100, 256 + 40], dtype=torch.int32, device="cuda")
+    other = hidden.clone()
+    other[1, 256 + 40:] = float("nan")
+    for x in (hidden, other):
+        layer.run(*halves(layer, x), cond, 0, lens)
+    assert torch.isfinite(hidden).all()
+    assert torch.equal(hidden[:, :256 + 40], other[:, :256 + 40]) and torch.equal(hidden[0], other[0])

@@ -229,3 +229,15 @@ def test_middling_products(size):
     """Fewer large tiles than the card has CUs, or not many more: 256 x 128 and 256 x 160."""
     test_large(size, True)
     test_large(size, False)
+
+
+@pytest.mark.parametrize("rows", [2, 90])
+def test_rows_that_are_one_row(rows):
+    """Inputs of stride 0: the same row of x for every token, the same residual for every sample or every token."""
+    one, w, b = normal((3, 1, 200), 1), normal((130, 200), 2, 200 ** -0.5), normal((130,), 3)
+    for r in (normal((1, rows, 130), 4).expand(3, -1, -1), normal((3, 1, 130), 5).expand(-1, rows, -1)):
+        out = torch.full((3, rows, 130), NAN, dtype=one.dtype, device="cuda")
+        ra.rapid_linear(one.expand(-1, rows, -1), w, out, b, "silu", b, r)
+        args = [widen(one.expand(-1, rows, -1)), widen(w), widen(b), "silu", widen(b.expand(3, -1)), widen(r)]
+        want = lo.linear(*args)
+        assert_within(out, want, bound(*args, want), str(rows))
