@@ -63,6 +63,7 @@ typedef enum {
  *   constraints  K a multiple of 8; x, w 16-byte aligned, their strides multiples of 8; y, residual, bias, gate 2-byte aligned;
  *             K <= w_stride <= 2^22; N <= 2^22; B*n < 2^31 - 256.  N, B and n may be anything (what is left of a row behind its
  *             last eight outputs is written element by element).  The rows of two consecutive samples of x (of 256, where n is small) lie within 2^30 elements.
+ * Fastest where rows of x and w start at multiples of 128 bytes and N is a multiple of 8.
  * y shares no byte with x, w, bias or gate, and none with residual but as above.
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE (sizes, strides); RAPID_ERR_UNSUPPORTED (K % 8, activation); RAPID_ERR_ALIGN;
  * RAPID_ERR_WORKSPACE (given, but too small or not aligned); RAPID_ERR_ALIAS (y starts where x, w, bias or gate does, or where
