@@ -325,8 +325,9 @@ bool rows_ok(const rapid_rows& a, int B, int n, int width, bool written, long lo
     sb = B == 1 ? 0 : a.stride_b;
     if (sn < 0 || sn > MAX_ROW_STRIDE || sb < 0 || sb > MAX_STRIDE) return false;
     if (!written) return true;
-    const long long rows = (n - 1) * sn + width, samples = (B - 1) * sb + width;
-    if (n > 1 && B > 1) return (sn >= width && sb >= rows) || (sb >= width && sn >= samples);
+    // apart: rows behind each other and samples behind each other, or samples within the rows' distance (sb <= sn <= 2^22 there:
+    // of larger ones a product by B could leave 64 bits)
+    if (n > 1 && B > 1) return (sn >= width && sb >= (n - 1) * sn + width) || (sb >= width && sb <= sn && sn >= (B - 1) * sb + width);
     return n > 1 ? sn >= width : B == 1 || sb >= width;
 }
 
