@@ -127,7 +127,7 @@ RAPID_API int rapid_rope_table(const int* positions, long long tokens, int n_axe
  * row t of the first or row t - n of the second).  Element (b, h, r, d) of q and k lies at ptr + b*in_stride_b + h*in_stride_h +
  * r*in_stride_n + d, of q_out and k_out at the out strides.
  * q_out may be q and k_out may be k, element for element (same pointer, same strides); else an output shares no byte with an
- * input or the other output.
+ * input or another output, those of the other segment included, and no two of its rows share an element.
  */
 typedef struct rapid_qk_segment {
     const void* q;
@@ -157,8 +157,10 @@ typedef enum {
  *   constraints  D 64 or 128; 16-byte aligned pointers (weights too); strides multiples of 8 elements, 0 <= stride_b, stride_h,
  *            stride_n <= 2^40 (those of dimensions of size 1 not looked at), out strides at least D; B*H <= 524287, N <= 2^22,
  *            B*N*ceil(H/2)*D <= 2^35 - 2048; table_stride_b a multiple of 4
- * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE; RAPID_ERR_UNSUPPORTED (D, rot, layout); RAPID_ERR_ALIGN; RAPID_ERR_ALIAS (q_out
- * starts where k_out or k does, k_out where q does, or an output where its input does with other strides); RAPID_ERR_DEVICE.
+ * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE (sizes, strides; rows of an output that share elements: a dimension of it is shorter
+ * than what those of smaller strides cover); RAPID_ERR_UNSUPPORTED (D, rot, layout); RAPID_ERR_ALIGN; RAPID_ERR_ALIAS (q_out
+ * starts where k_out or k does, k_out where q does, an output where its input does with other strides, or where a tensor of the
+ * other segment does); RAPID_ERR_DEVICE.
  */
 RAPID_API int rapid_qk_norm_rope(const rapid_qk_segment* segments, int n_segments, int B, int H, int D, float eps,
                                  const float* table, long long table_stride_b, int rot, int layout, void* stream);

@@ -331,6 +331,25 @@ bool rows_ok(const rapid_rows& a, int B, int n, int width, bool written, long lo
     return n > 1 ? sn >= width : B == 1 || sb >= width;
 }
 
+// Whether no two rows of D elements of an output share one: the dimensions by their strides, each at least as far as those within reach.
+bool rows_apart(const int (&sizes)[3], const long long (&strides)[3], int D)
+{
+    int order[3] = {0, 1, 2};
+    for (int i = 1; i < 3; ++i)
+        for (int j = i; j > 0 && strides[order[j]] < strides[order[j - 1]]; --j) {
+            const int k = order[j];
+            order[j] = order[j - 1];
+            order[j - 1] = k;
+        }
+    long long reach = D;
+    for (int i : order) {
+        if (sizes[i] == 1) continue;
+        if (strides[i] < reach) return false;
+        reach += (sizes[i] - 1) * strides[i];
+    }
+    return true;
+}
+
 template <int WAVES, int CHUNKS>
 int launch_modulate(const ModulateParams& p, void* stream)
 {
@@ -396,6 +415,15 @@ int qk_rows(const rapid_qk_segment* segments, int n_segments, int B, int H, int 
         N += g.n;
     }
     if (N > (1 << 22)) return RAPID_ERR_SHAPE;
+    for (int i = 0; i < n_segments; ++i) {
+        const int sizes[3] = {B, H, segments[i].n};
+        const long long strides[3] = {p.out_sb[i], p.out_sh[i], p.out_sn[i]};
+        if (!rows_apart(sizes, strides, D)) return RAPID_ERR_SHAPE;
+        if (n_segments == 1) break;
+        const rapid_qk_segment &g = segments[i], &o = segments[1 - i];
+        for (const void* out : {g.q_out, g.k_out})
+            if (out == o.q || out == o.k || out == o.q_out || out == o.k_out) return RAPID_ERR_ALIAS;
+    }
     if (table) {
         if (rot <= 0 || rot > D || rot % 16 != 0 || layout < RAPID_ROPE_INTERLEAVED || layout > RAPID_ROPE_HALVES) return RAPID_ERR_UNSUPPORTED;
         p.table_sb = B == 1 ? 0 : table_stride_b;
