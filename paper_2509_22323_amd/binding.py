@@ -196,7 +196,7 @@ def _load_native():
     module.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "rapid_attn_dense", "rapid_attn_block_sparse", "rapid_attn_joint", "rapid_attn_joint_select", "rapid_mask_select",
         "rapid_cache_store", "rapid_cache_reuse", "rapid_linear", "rapid_linear_workspace_bytes", "rapid_norm_modulate",
-        "rapid_rope_table", "rapid_qk_norm_rope", "rapid_rope")))
+        "rapid_rope_table", "rapid_qk_norm_rope", "rapid_rope")), RopeAxis)
     _native = module
     return module
 
@@ -711,6 +711,8 @@ def rapid_rope_table(positions, axes, table, magnitude=1.0):
             and table.dim() >= 3):
         raise TypeError("table must be a contiguous CUDA float32 tensor [...,rot/2,2]")
     axes = list(axes)
+    if not all(isinstance(a, RopeAxis) for a in axes):
+        raise TypeError("axes must be RopeAxis descriptors")
     pairs = sum(int(a.dim) for a in axes) // 2
     device = positions.get_device()
     if table.get_device() != device:

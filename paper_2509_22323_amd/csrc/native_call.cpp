@@ -21,6 +21,7 @@
 namespace {
 
 PyObject* current_stream = nullptr;                // torch._C._cuda_getCurrentRawStream
+PyObject* axis_type = nullptr;                     // RopeAxis of binding.py, a rapid_rope_axis in a buffer
 
 decltype(&rapid_attn_dense) attn_dense;
 decltype(&rapid_attn_block_sparse) attn_block_sparse;
@@ -387,7 +388,7 @@ PyObject* modulate(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// (positions, axes: a list or tuple of rapid_rope_axis, table, magnitude)
+// (positions, axes: a list or tuple of RopeAxis, table, magnitude)
 PyObject* table(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     if (n != 4 || (!PyList_CheckExact(a[1]) && !PyTuple_CheckExact(a[1]))) Py_RETURN_NONE;
@@ -402,7 +403,7 @@ PyObject* table(PyObject*, PyObject* const* a, Py_ssize_t n)
     for (Py_ssize_t i = 0; i < axes; ++i) {
         Py_buffer b;
         PyObject* o = PySequence_Fast_GET_ITEM(a[1], i);
-        if (!PyObject_CheckBuffer(o)) Py_RETURN_NONE;
+        if (!PyType_IsSubtype(Py_TYPE(o), (PyTypeObject*)axis_type)) Py_RETURN_NONE;
         if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) { PyErr_Clear(); Py_RETURN_NONE; }
         const bool fits = b.len == (Py_ssize_t)sizeof(rapid_rope_axis);
         if (fits) memcpy(&axis[i], b.buf, sizeof(rapid_rope_axis));
@@ -501,11 +502,12 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n)
     return launch(x.device, [&](void* s) { return layer_rope(x.seg, x.n, x.B, x.H, x.D, x.table, x.table_stride, x.rot, x.layout, s); });
 }
 
-// bind(address of each entry point, ..): of the library that binding.py has loaded
+// bind(address of each entry point, .., RopeAxis): of the library that binding.py has loaded
 PyObject* bind(PyObject*, PyObject* args)
 {
     unsigned long long p[13];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12])) return nullptr;
+    PyTypeObject* axis;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKO!", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12], &PyType_Type, &axis)) return nullptr;
     attn_dense = (decltype(attn_dense))p[0];
     attn_block_sparse = (decltype(attn_block_sparse))p[1];
     attn_joint = (decltype(attn_joint))p[2];
@@ -519,6 +521,8 @@ PyObject* bind(PyObject*, PyObject* args)
     layer_table = (decltype(layer_table))p[10];
     layer_qk = (decltype(layer_qk))p[11];
     layer_rope = (decltype(layer_rope))p[12];
+    Py_INCREF(axis);
+    Py_XSETREF(axis_type, (PyObject*)axis);
     PyObject* c = PyImport_ImportModule("torch._C");
     if (!c) return nullptr;
     Py_XSETREF(current_stream, PyObject_GetAttrString(c, "_cuda_getCurrentRawStream"));

@@ -1,0 +1,32 @@
+"""Calls of the operators around the attention that their documentation allows or excludes, in both forms of the binding."""
+import pytest
+import torch
+
+import paper_2509_22323_amd as ra
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=["native", "python"])
+def form(request, monkeypatch):
+    if request.param == "python":
+        monkeypatch.setattr(ra.binding, "_native", ra.binding._NoNative())
+    return request.param
+
+
+def test_axes_are_descriptors(form):
+    """A buffer of a descriptor's size is none, nor is something with its attributes."""
+    class Alike:
+        dim = 64
+
+    positions, table = torch.zeros((9, 1), dtype=torch.int32, device="cuda"), torch.empty(9, 32, 2, device="cuda")
+    axis = ra.RopeAxis(64)
+    for other in (bytes(axis), bytearray(axis), memoryview(bytes(axis)), Alike(), 64, None):
+        with pytest.raises(TypeError):
+            ra.rapid_rope_table(positions, [other], table)
+
+    class Named(ra.RopeAxis):
+        pass
+
+    want = ra.rapid_rope_table(positions + 3, [axis], torch.empty_like(table))
+    assert torch.equal(ra.rapid_rope_table(positions + 3, [Named(64)], table), want)
