@@ -66,12 +66,19 @@ bool integer(PyObject* o, int& v)
     v = (int)x;
     return true;
 }
-bool number(PyObject* o, float& v)
+bool number(PyObject* o, double& v)
 {
-    if (PyFloat_CheckExact(o)) { v = (float)PyFloat_AS_DOUBLE(o); return true; }
+    if (PyFloat_CheckExact(o)) { v = PyFloat_AS_DOUBLE(o); return true; }
     int i;
     if (!integer(o, i)) return false;
-    v = (float)i;
+    v = i;
+    return true;
+}
+bool number(PyObject* o, float& v)
+{
+    double d;
+    if (!number(o, d)) return false;
+    v = (float)d;
     return true;
 }
 bool size(int64_t n, int& v)
@@ -394,7 +401,7 @@ PyObject* table(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (n != 4 || (!PyList_CheckExact(a[1]) && !PyTuple_CheckExact(a[1]))) Py_RETURN_NONE;
     const at::Tensor *p = of(a[0], at::kInt), *t = of(a[2], at::kFloat);
     const Py_ssize_t axes = PySequence_Fast_GET_SIZE(a[1]);
-    float magnitude;
+    double magnitude;
     if (!p || !t || axes < 1 || axes > 8 || !p->is_contiguous() || !t->is_contiguous() || t->get_device() != p->get_device()) Py_RETURN_NONE;
     if (!current(p->get_device()) || p->dim() < 2 || t->dim() != p->dim() + 1 || p->size(-1) != axes || t->size(-1) != 2) Py_RETURN_NONE;
     if (p->sizes().slice(0, p->dim() - 1) != t->sizes().slice(0, t->dim() - 2) || !number(a[3], magnitude)) Py_RETURN_NONE;
@@ -415,8 +422,7 @@ PyObject* table(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int* positions = (const int*)p->data_ptr();
     float* out = (float*)t->data_ptr();
     const long long tokens = p->numel() / axes;
-    const double scale = PyFloat_CheckExact(a[3]) ? PyFloat_AS_DOUBLE(a[3]) : (double)magnitude;
-    return launch(p->get_device(), [&](void* s) { return layer_table(positions, tokens, (int)axes, axis, scale, out, s); });
+    return launch(p->get_device(), [&](void* s) { return layer_table(positions, tokens, (int)axes, axis, magnitude, out, s); });
 }
 
 // (segments of (q, k, q_out, k_out), weights or None, table or None, layout): both forms

@@ -30,3 +30,11 @@ def test_axes_are_descriptors(form):
 
     want = ra.rapid_rope_table(positions + 3, [axis], torch.empty_like(table))
     assert torch.equal(ra.rapid_rope_table(positions + 3, [Named(64)], table), want)
+
+
+def test_magnitudes_that_are_whole_numbers(form):
+    """(2^24 + 1 and its like are no fp32)"""
+    positions = torch.arange(64, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    for magnitude in (3, -2, (1 << 24) + 1, (1 << 25) + 3, (1 << 40) + 12345):
+        got, want = (ra.rapid_rope_table(positions, [ra.RopeAxis(64)], torch.empty(64, 32, 2, device="cuda"), kind(magnitude)) for kind in (int, float))
+        assert torch.equal(got, want), magnitude
