@@ -17,6 +17,35 @@ WEIGHTS = ("mod_w", "mod_b",           # [6C, C]: shift, scale, gate of the atte
            "ff_out_w", "ff_out_b")     # [C, F]
 
 
+_NONE_ALLOWED = ("mod_b", "qkv_b", "q_norm", "k_norm", "out_b", "ff_in_b", "ff_out_b")
+
+
+def _check_sizes(weights, B, H, D, image, text, layout, eps):
+    """What a run would refuse half way through it."""
+    if B < 1 or H < 1 or D not in (64, 128):
+        raise ValueError(f"B = {B}, H = {H}, D = {D}: D is 64 or 128, B and H are at least 1")
+    if image < 128 or image % 128 != 0:
+        raise ValueError(f"{image} image tokens: their number must be a multiple of 128")
+    if text < 1:
+        raise ValueError(f"{text} text tokens: there must be one at least")
+    if layout not in _b.ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(_b.ROPE_LAYOUTS)}")
+    if not eps >= 0:
+        raise ValueError("eps must not be negative")
+    if len(weights) != 2:
+        raise ValueError("weights: of the image stream and of the text stream")
+    C = H * D
+    for stream, w in zip(("image", "text"), weights):
+        F = w["ff_in_w"].shape[0]
+        if F < 8 or F % 8 != 0:
+            raise ValueError(f"{stream} stream: {F} channels of the feed-forward block, not a multiple of 8")
+        for name, shape in zip(WEIGHTS, ((6 * C, C), (6 * C,), (3 * C, C), (3 * C,), (D,), (D,), (C, C), (C,), (F, C), (F,), (C, F), (C,))):
+            if w[name] is None and name in _NONE_ALLOWED:
+                continue
+            if w[name] is None or tuple(w[name].shape) != shape:
+                raise ValueError(f"{stream} stream: {name} must be {list(shape)}, not {None if w[name] is None else list(w[name].shape)}")
+
+
 class JointLayer:
     """weights: (of the image stream, of the text stream), each a dict of CUDA bf16 tensors named as in WEIGHTS (biases and norms
     may be None).  positions (CUDA int32 [image + text, axes]) and axes (RopeAxis each): the rotation of queries and keys; None =
@@ -24,6 +53,7 @@ class JointLayer:
 
     def __init__(self, weights, B, H, D, image, text, positions=None, axes=None, layout="interleaved", eps=1e-6):
         import torch
+        _check_sizes(weights, B, H, D, image, text, layout, eps)
         self.weights, self.B, self.H, self.D, self.layout, self.eps = weights, B, H, D, layout, eps
         self.tokens = (image, text)
         device = weights[0]["qkv_w"].device
@@ -52,6 +82,8 @@ class JointLayer:
     def run(self, image, text, conditioning, a_sparse=0, kv_lens=None):
         """image [B, n, C], text [B, m, C] <- the layer's output, in place.  conditioning: [B, C], the vector that every layer's
         projection takes (its activation done); a_sparse: the Sparse-Attention action (0: dense); kv_lens as rapid_attn_joint."""
+        if int(a_sparse) not in range(4):
+            raise ValueError(f"a_sparse = {a_sparse}: the Sparse-Attention actions are 0 to 3")
         hidden = (image, text)
         for x, h, mod, qkv, w in zip(hidden, self.h, self.mod, self.qkv, self.weights):
             _b.rapid_linear(conditioning, w["mod_w"], mod.view(self.B, -1), w["mod_b"], workspace=self.workspace)

@@ -1,0 +1,50 @@
+"""Host-only checks of layer.JointLayer: sizes and weights that a run would refuse half way through are refused when it is made."""
+import pytest
+import torch
+
+import paper_2509_22323_amd as ra
+from paper_2509_22323_amd import layer as layer_module
+
+SIZES = dict(B=2, H=2, D=64, image=256, text=9)
+
+
+def weights(C=128, D=64, F=136, **other):
+    """(zeros on the CPU: enough for what is checked before any call)"""
+    shapes = dict(mod_w=(6 * C, C), mod_b=(6 * C,), qkv_w=(3 * C, C), qkv_b=(3 * C,), q_norm=(D,), k_norm=(D,), out_w=(C, C), out_b=(C,),
+                  ff_in_w=(F, C), ff_in_b=(F,), ff_out_w=(C, F), ff_out_b=(C,))
+    assert set(shapes) == set(layer_module.WEIGHTS)
+    shapes.update(other)
+    return {k: None if s is None else torch.zeros(s, dtype=torch.bfloat16) for k, s in shapes.items()}
+
+
+def make(first=None, second=None, **kw):
+    return ra.JointLayer((first or weights(), second or weights(F=64)), **{**SIZES, **kw})
+
+
+def test_a_layer_is_made_on_the_weights_device():
+    layer = make(weights(mod_b=None, qkv_b=None, q_norm=None, k_norm=None, out_b=None, ff_in_b=None, ff_out_b=None))
+    assert [tuple(t.shape) for t in layer.f] == [(2, 256, 136), (2, 9, 64)]
+
+
+@pytest.mark.parametrize("kw", [
+    dict(image=200), dict(image=64), dict(image=0), dict(image=-128), dict(text=0), dict(text=-5), dict(B=0), dict(H=0), dict(H=1, D=128), dict(D=32),
+    dict(D=96), dict(layout="halves"), dict(eps=-1e-6), dict(eps=float("nan")), dict(first=weights(F=132)), dict(second=weights(F=4)),
+    dict(second=weights(C=64)), dict(first=weights(D=32)), dict(first=weights(mod_w=(5 * 128, 128))), dict(first=weights(qkv_w=(128, 384))),
+    dict(second=weights(out_w=None)), dict(second=weights(ff_out_b=(136,))), dict(second=weights(ff_out_w=(128, 64)))], ids=lambda kw: " ".join(kw))
+def test_sizes_that_do_not_fit(kw):
+    with pytest.raises(ValueError):
+        make(**kw)
+
+
+def test_one_stream_is_no_layer():
+    with pytest.raises(ValueError):
+        ra.JointLayer((weights(),), **SIZES)
+
+
+@pytest.mark.parametrize("a_sparse", [-1, 4, 17])
+def test_actions_that_there_are_not(a_sparse, monkeypatch):
+    """refused before anything is called"""
+    layer = make()
+    monkeypatch.setattr(layer_module, "_b", None)
+    with pytest.raises(ValueError):
+        layer.run(torch.zeros(2, 256, 128), torch.zeros(2, 9, 128), torch.zeros(2, 128), a_sparse)
