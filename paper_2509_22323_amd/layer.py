@@ -57,6 +57,7 @@ class JointLayer:
         self.weights, self.B, self.H, self.D, self.layout, self.eps = weights, B, H, D, layout, eps
         self.tokens = (image, text)
         device = weights[0]["qkv_w"].device
+        self.device = device.index
         C, wide = H * D, [w["ff_in_w"].shape[0] for w in weights]
 
         def empty(*shape, dtype=torch.bfloat16):
@@ -84,6 +85,13 @@ class JointLayer:
         projection takes (its activation done); a_sparse: the Sparse-Attention action (0: dense); kv_lens as rapid_attn_joint."""
         if int(a_sparse) not in range(4):
             raise ValueError(f"a_sparse = {a_sparse}: the Sparse-Attention actions are 0 to 3")
+        import torch
+        if torch._C._cuda_getDevice() == self.device:
+            return self._run(image, text, conditioning, a_sparse, kv_lens)
+        with torch.cuda.device(self.device):               # (the attention calls launch on the current device)
+            return self._run(image, text, conditioning, a_sparse, kv_lens)
+
+    def _run(self, image, text, conditioning, a_sparse, kv_lens):
         hidden = (image, text)
         for x, h, mod, qkv, w in zip(hidden, self.h, self.mod, self.qkv, self.weights):
             _b.rapid_linear(conditioning, w["mod_w"], mod.view(self.B, -1), w["mod_b"], workspace=self.workspace)

@@ -34,7 +34,8 @@ def run_action_trace(trace, q, k, v, o, n_layers, block, kv_len, text_start, x, 
     step starts from x and leaves its result in out."""
     import torch
     if layer is not None:
-        return _run_layer_trace(trace, layer, conditioning, n_layers, x, delta, out)
+        with torch.cuda.device(layer.device):              # events and the residual's calls belong to the current one
+            return _run_layer_trace(trace, layer, conditioning, n_layers, x, delta, out)
     B, H, N, D = (int(s) for s in q.shape)
     nb = N // block
     res = TraceResult(calls={"rapid_attn_dense": 0, "rapid_attn_block_sparse": 0, "rapid_mask_select": 0,

@@ -48,3 +48,50 @@ def test_actions_that_there_are_not(a_sparse, monkeypatch):
     monkeypatch.setattr(layer_module, "_b", None)
     with pytest.raises(ValueError):
         layer.run(torch.zeros(2, 256, 128), torch.zeros(2, 9, 128), torch.zeros(2, 128), a_sparse)
+
+
+class Current:
+    """Stands in for torch's current device: 0, or what the innermost `with` names."""
+    def __init__(self, monkeypatch):
+        self.device = 0
+        current = self
+
+        class Guard:
+            def __init__(self, device):
+                self.to = device
+
+            def __enter__(self):
+                self.before, current.device = current.device, self.to
+
+            def __exit__(self, *_):
+                current.device = self.before
+
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current.device, raising=False)
+        monkeypatch.setattr(torch.cuda, "device", Guard)
+
+
+@pytest.mark.parametrize("device", [0, 1])
+@pytest.mark.parametrize("a_sparse", [0, 3])
+def test_calls_are_made_with_the_layers_device_current(device, a_sparse, monkeypatch):
+    """The calls that launch on the current device find the layer's one there, and the caller's is current again behind a run."""
+    layer, current, made = make(), Current(monkeypatch), []
+    layer.device = device
+
+    class Calls:
+        def __getattr__(self, name):
+            return lambda *a, **k: made.append((name, current.device))
+
+    monkeypatch.setattr(layer_module, "_b", Calls())
+    layer.run(torch.zeros(2, 256, 128), torch.zeros(2, 9, 128), torch.zeros(2, 128), a_sparse)
+    assert current.device == 0 and {d for _, d in made} == {device}
+    attention = "rapid_attn_joint" if a_sparse == 0 else "rapid_attn_joint_select"
+    assert [name for name, _ in made].count(attention) == 1 and len([1 for name, _ in made if name == "rapid_linear"]) == 10
+
+
+def test_a_trace_is_played_with_the_layers_device_current(monkeypatch):
+    from paper_2509_22323_amd import sampler
+    layer, current, made = make(), Current(monkeypatch), []
+    layer.device = 1
+    monkeypatch.setattr(sampler, "_run_layer_trace", lambda *a: made.append(current.device))
+    sampler.run_action_trace([(0, 0)], None, None, None, None, 1, 128, None, None, None, None, None, layer=layer)
+    assert made == [1] and current.device == 0
