@@ -34,6 +34,8 @@ def run_action_trace(trace, q, k, v, o, n_layers, block, kv_len, text_start, x, 
     step starts from x and leaves its result in out."""
     import torch
     if layer is not None:
+        if len({x.data_ptr(), delta.data_ptr(), out.data_ptr()}) != 3:
+            raise ValueError("x, delta and out must be tensors of their own: layers run in out, and the residual is its distance from x")
         with torch.cuda.device(layer.device):              # events and the residual's calls belong to the current one
             return _run_layer_trace(trace, layer, conditioning, n_layers, x, delta, out)
     B, H, N, D = (int(s) for s in q.shape)

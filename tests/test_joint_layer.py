@@ -93,5 +93,15 @@ def test_a_trace_is_played_with_the_layers_device_current(monkeypatch):
     layer, current, made = make(), Current(monkeypatch), []
     layer.device = 1
     monkeypatch.setattr(sampler, "_run_layer_trace", lambda *a: made.append(current.device))
-    sampler.run_action_trace([(0, 0)], None, None, None, None, 1, 128, None, None, None, None, None, layer=layer)
+    sampler.run_action_trace([(0, 0)], None, None, None, None, 1, 128, None, None, *torch.zeros(3, 2, 8), layer=layer)
     assert made == [1] and current.device == 0
+
+
+@pytest.mark.parametrize("which", [(0, 0, 0), (0, 1, 0), (0, 0, 1), (0, 1, 1)], ids=str)
+def test_a_trace_of_layers_needs_tensors_of_its_own(which, monkeypatch):
+    from paper_2509_22323_amd import sampler
+    Current(monkeypatch)
+    monkeypatch.setattr(sampler, "_run_layer_trace", lambda *a: pytest.fail("played"))
+    t = torch.zeros(2, 2, 8)
+    with pytest.raises(ValueError):
+        sampler.run_action_trace([(0, 0)], None, None, None, None, 1, 128, None, None, *(t[i] for i in which), layer=make())
