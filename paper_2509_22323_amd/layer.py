@@ -48,8 +48,8 @@ def _check_sizes(weights, B, H, D, image, text, layout, eps):
 
 class JointLayer:
     """weights: (of the image stream, of the text stream), each a dict of CUDA bf16 tensors named as in WEIGHTS (biases and norms
-    may be None).  positions (CUDA int32 [image + text, axes]) and axes (RopeAxis each): the rotation of queries and keys; None =
-    none.  image is a multiple of 128, F of 8."""
+    may be None).  positions (CUDA int32 [image + text, axes], or [B, image + text, axes]) and axes (RopeAxis each): the rotation
+    of queries and keys; None = none.  image is a multiple of 128, F of 8."""
 
     def __init__(self, weights, B, H, D, image, text, positions=None, axes=None, layout="interleaved", eps=1e-6):
         import torch
@@ -70,7 +70,9 @@ class JointLayer:
         self.f = [empty(B, n, F) for n, F in zip(self.tokens, wide)]
         self.table = None
         if positions is not None:
-            self.table = empty(image + text, sum(int(a.dim) for a in axes) // 2, 2, dtype=torch.float32)
+            if tuple(positions.shape) not in ((image + text, len(axes)), (B, image + text, len(axes))):
+                raise ValueError(f"positions must be [{image + text}, {len(axes)}] or [{B}, {image + text}, {len(axes)}], not {list(positions.shape)}")
+            self.table = empty(*positions.shape[:-1], sum(int(a.dim) for a in axes) // 2, 2, dtype=torch.float32)
             _b.rapid_rope_table(positions, axes, self.table)
         need = max(_b.rapid_linear_workspace_bytes(M, N, K) for n, F in zip(self.tokens, wide)
                    for M, N, K in ((B, 6 * C, C), (B * n, 3 * C, C), (B * n, C, C), (B * n, F, C), (B * n, C, F)))

@@ -38,3 +38,24 @@ def test_magnitudes_that_are_whole_numbers(form):
     for magnitude in (3, -2, (1 << 24) + 1, (1 << 25) + 3, (1 << 40) + 12345):
         got, want = (ra.rapid_rope_table(positions, [ra.RopeAxis(64)], torch.empty(64, 32, 2, device="cuda"), kind(magnitude)) for kind in (int, float))
         assert torch.equal(got, want), magnitude
+
+
+def test_a_layer_with_positions_for_every_sample():
+    """Each sample as a layer with its positions alone leaves it."""
+    from test_gpu_joint_layer import halves, make
+    layer, hidden, cond = make(text=40, seed=15)
+    B, (image, text) = layer.B, layer.tokens
+    axes = [ra.RopeAxis(16), ra.RopeAxis(24), ra.RopeAxis(24)]
+    t = torch.arange(image + text, dtype=torch.int32, device="cuda")
+    both = torch.stack([torch.stack([0 * t, t // w, t % w], -1) for w in (16, 32)])
+    start, want = hidden.clone(), []
+    for positions in both:
+        one = ra.JointLayer(layer.weights, B, layer.H, layer.D, image, text, positions.contiguous(), axes)
+        hidden.copy_(start)
+        one.run(*halves(one, hidden), cond)
+        want.append(hidden.clone())
+    each = ra.JointLayer(layer.weights, B, layer.H, layer.D, image, text, both, axes)
+    hidden.copy_(start)
+    each.run(*halves(each, hidden), cond)
+    assert not torch.equal(want[0][1], want[1][1])
+    assert torch.equal(hidden[0], want[0][0]) and torch.equal(hidden[1], want[1][1])

@@ -36,6 +36,12 @@ def test_sizes_that_do_not_fit(kw):
         make(**kw)
 
 
+@pytest.mark.parametrize("shape", [(264, 2), (265, 1), (265, 3), (1, 265, 2), (3, 265, 2), (2, 264, 2), (2, 1, 265, 2), (265,)], ids=str)
+def test_positions_that_do_not_fit(shape):
+    with pytest.raises(ValueError):
+        make(positions=torch.zeros(shape, dtype=torch.int32), axes=[ra.RopeAxis(32), ra.RopeAxis(32)])
+
+
 def test_one_stream_is_no_layer():
     with pytest.raises(ValueError):
         ra.JointLayer((weights(),), **SIZES)
