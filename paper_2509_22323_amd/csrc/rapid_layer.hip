@@ -281,7 +281,7 @@ struct TableParams {
 };
 
 // magnitude * (cos, sin) of a number of turns, in fp64 as far as fp32 can tell: taken to the nearest quarter, where Taylor's sums of
-// six and five terms are off by 1.1e-10 (cosine) and 1.8e-9 (sine) at most, 0.03 of half a step of fp32.  (With the library's
+// six and five terms are off by 1.1e-10 (cosine) and 1.8e-9 (sine) at most, 0.06 of half a step of fp32.  (With the library's
 // fp64 sincospi 264 K tokens of 64 pairs take 62 us, stores of 8 bytes and a 64-bit division a pair included.)
 __device__ __forceinline__ float2 turned(double turns, double magnitude)
 {

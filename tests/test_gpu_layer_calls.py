@@ -1,8 +1,10 @@
 """Calls of the operators around the attention that their documentation allows or excludes, in both forms of the binding."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2509_22323_amd as ra
+from layer_common import assert_within
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +61,22 @@ def test_a_layer_with_positions_for_every_sample():
     each.run(*halves(each, hidden), cond)
     assert not torch.equal(want[0][1], want[1][1])
     assert torch.equal(hidden[0], want[0][0]) and torch.equal(hidden[1], want[1][1])
+
+
+@pytest.mark.parametrize("dim,theta", [(64, 10000.0), (128, 500000.0), (16, 3.0)])
+@pytest.mark.parametrize("far", [1 << 8, 1 << 16, 1 << 26, (1 << 31) - 1])
+@pytest.mark.parametrize("magnitude", [1.0, -1.375])
+def test_table_is_as_exact_as_its_documentation_says(dim, theta, far, magnitude):
+    """Half a step of fp32, 2^-29 for the sums of sine and cosine, 2^-52 of the angle (its frequency and its product, half a step of
+    fp64 each).  The reference's angles have 64 bits: 2^-63 |a| more, and its numbers are rounded to fp64."""
+    rng = np.random.default_rng(dim)
+    p = np.concatenate([rng.integers(-far, far, 500), [0, 1, -1, far - 1, -far]]).astype(np.int32)
+    table = ra.rapid_rope_table(torch.from_numpy(p).cuda()[:, None].contiguous(), [ra.RopeAxis(dim, theta)],
+                                torch.empty(p.size, dim // 2, 2, device="cuda"), magnitude)
+    assert np.finfo(np.longdouble).nmant >= 63
+    f = np.longdouble(theta) ** (-np.arange(0, dim, 2).astype(np.longdouble) / dim)
+    a = p[:, None].astype(np.longdouble) * f
+    want = (magnitude * np.stack([np.cos(a), np.sin(a)], -1)).astype(np.float64)
+    own = abs(magnitude) * (2.0 ** -29 + (2.0 ** -52 + 2.0 ** -61) * np.abs(a).astype(np.float64))[..., None]
+    step = np.spacing((np.abs(want) + own).astype(np.float32)).astype(np.float64)
+    assert_within(table, want, own + step / 2 + 2.0 ** -52 * np.abs(want))
