@@ -11,8 +11,10 @@
  *   rapid_rope_table      the cosines and sines both read, from positions over several axes
  *
  * All tensors are bf16 but for the table (fp32) and the positions (int32); arithmetic is fp32 (the product: bf16 MFMA with
- * fp32 accumulation; angles: fp64) and every result is rounded once, to nearest even.  These are operators of inference, as
- * all of this library: there are no gradients.
+ * fp32 accumulation; angles: fp64) and every result is rounded once, to nearest even.  Norms take squares in fp32: a row whose
+ * squares (of rapid_norm_modulate: of whose deviations) add up to 2^128 or more, elements of 2^60 in a row of 256 say, is zeros
+ * behind the norm, or NaN where its elements add up to that; with eps = 0 one of a mean square below 2^-126 is infinities or NaN.
+ * These are operators of inference, as all of this library: there are no gradients.
  *
  * Memory: device pointers are the caller's; descriptors (structs, arrays of them) are HOST memory, read during the call.  The
  * library allocates nothing, keeps no state between calls and never synchronises: kernels are enqueued on `stream` (a
@@ -64,6 +66,9 @@ typedef enum {
  *             K <= w_stride <= 2^22; N <= 2^22; B*n < 2^31 - 256.  N, B and n may be anything (what is left of a row behind its
  *             last eight outputs is written element by element).  The rows of two consecutive samples of x (of 256, where n is small) lie within 2^30 elements.
  * Fastest where rows of x and w start at multiples of 128 bytes and N is a multiple of 8.
+ * The same call gives the same bits, whenever it is made.  The order in which a sum's K terms are added is another for other sizes,
+ * with or without a workspace, and in other tiles of one product: equal rows of x, in one call or in calls of other sizes, can
+ * give outputs that differ by what fp32 sums in another order differ by.
  * y shares no byte with x, w, bias or gate, and none with residual but as above.
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE (sizes, strides); RAPID_ERR_UNSUPPORTED (K % 8, activation); RAPID_ERR_ALIGN;
  * RAPID_ERR_WORKSPACE (given, but too small or not aligned); RAPID_ERR_ALIAS (y starts where x, w, bias or gate does, or where

@@ -575,6 +575,7 @@ def rapid_attn_joint_select(segments, block=128, kv_len=None, kv_lens=None, text
 
 
 # ---------------------------------------------------------------- a layer around its attention
+# Operators of inference: none of them is recorded by autograd, whatever its tensors require, and there are no gradients.
 _LAYER_ERRORS = {
     -1: "a required pointer is NULL",
     -2: "invalid shape: a size or stride out of range, or rows of an output that share elements",
@@ -635,7 +636,8 @@ def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residu
     """out <- residual + gate * act(x weight^T + bias).  x [B,n,K] (or [n,K]), out and residual [B,n,N]: CUDA bf16, last dimension
     contiguous; weight [N,K]; bias [N]; gate [B,N] or [N]; activation "none", "silu" or "gelu_tanh".  residual may be out.
     `workspace`: CUDA uint8 tensor of at least rapid_linear_workspace_bytes(B*n, N, K) bytes; allocated with torch if None.
-    Returns out."""
+    The same call gives the same bits; equal rows of x need not, their sums can be taken in another order.
+    Inference only: not recorded by autograd, no gradients.  Returns out."""
     status = (_native or _load_native()).linear(x, weight, out, bias, activation, gate, residual, workspace)
     if status is not None:
         _check_layer(status)
@@ -676,7 +678,8 @@ def rapid_linear(x, weight, out, bias=None, activation="none", gate=None, residu
 
 def rapid_norm_modulate(x, out, scale=None, shift=None, eps=1e-6):
     """out <- (x - mean) / sqrt(variance + eps) * (1 + scale) + shift over the last dimension.  x, out [B,n,C] (or [n,C]): CUDA
-    bf16, last dimension contiguous; scale, shift [B,C] or [C], both or neither.  out may be x.  Returns out."""
+    bf16, last dimension contiguous; scale, shift [B,C] or [C], both or neither.  out may be x.
+    Inference only: not recorded by autograd, no gradients.  Returns out."""
     status = (_native or _load_native()).modulate(x, out, scale, shift, eps)
     if status is not None:
         _check_layer(status)
@@ -782,7 +785,8 @@ def rapid_qk_norm_rope(segments, weights=None, table=None, layout="interleaved",
     k_out), each CUDA bf16 indexed [B, H, n, D] with a contiguous last dimension and any other strides; q and k share theirs,
     q_out and k_out theirs; q_out may be q and k_out k.  weights: a (q_weight, k_weight) for each segment, [D] or None;
     table: float32 [N, rot/2, 2] (rapid_rope_table) over the joint tokens, or [B, N, rot/2, 2], or None: the norm alone;
-    layout "interleaved" or "half".  Returns the outputs, (q_out, k_out) of one segment after the other."""
+    layout "interleaved" or "half".  Inference only: not recorded by autograd, no gradients.
+    Returns the outputs, (q_out, k_out) of one segment after the other."""
     status = (_native or _load_native()).qk_norm_rope(segments, weights, table, layout, eps)
     if status is not None:
         _check_layer(status)
@@ -794,7 +798,7 @@ def rapid_qk_norm_rope(segments, weights=None, table=None, layout="interleaved",
 
 
 def rapid_rope(segments, table, layout="interleaved"):
-    """The rotation of rapid_qk_norm_rope alone.  Returns the outputs."""
+    """The rotation of rapid_qk_norm_rope alone.  Inference only: not recorded by autograd, no gradients.  Returns the outputs."""
     status = (_native or _load_native()).rope(segments, None, table, layout)
     if status is not None:
         _check_layer(status)

@@ -2,6 +2,7 @@
 weights of its own, joined for attention alone; every projection under the conditioning of the time step).
 
 Weights are the caller's (there are none here); buffers are made once, a run allocates nothing and can be captured into a graph.
+Inference only: runs are not recorded by autograd, whatever the weights require.
 Runs of one layer, graphs of them included, share its buffers: they follow each other, on the stream that it was made on or behind it.
 """
 from __future__ import annotations

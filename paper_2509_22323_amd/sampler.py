@@ -7,8 +7,8 @@ X + Delta; a computing step runs every layer's joint attention, dense for sparse
 block-sparse under the selected mask for actions 1..3, and then refreshes the cached residual).
 The same Q/K/V stand in for every layer.  With a `layer` (layer.JointLayer) a computing step runs the
 whole layer instead, projections, norms and rotation included, on hidden states; one layer's weights stand
-in for all.  All work is library calls on torch's current stream; this module only sequences them and reads
-HIP events.
+in for all.  All work is library calls on torch's current stream (and with a layer a copy of x to out before a
+computing step's layers, which run in place); this module only sequences them and reads HIP events.
 """
 from __future__ import annotations
 

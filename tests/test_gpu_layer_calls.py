@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2509_22323_amd as ra
-from layer_common import assert_within
+from layer_common import BF16_STEP, assert_within, normal, widen
 
 pytestmark = pytest.mark.gpu
 
@@ -80,3 +80,43 @@ def test_table_is_as_exact_as_its_documentation_says(dim, theta, far, magnitude)
     own = abs(magnitude) * (2.0 ** -29 + (2.0 ** -52 + 2.0 ** -61) * np.abs(a).astype(np.float64))[..., None]
     step = np.spacing((np.abs(want) + own).astype(np.float32)).astype(np.float64)
     assert_within(table, want, own + step / 2 + 2.0 ** -52 * np.abs(want))
+
+
+def test_tensors_that_require_gradients_are_taken_and_nothing_is_recorded(form):
+    x, w = normal((2, 9, 64), 1), normal((40, 64), 2, 0.125)
+    q = normal((2, 1, 2, 9, 64), 3)
+    table = ra.rapid_rope_table(torch.arange(9, dtype=torch.int32, device="cuda")[:, None].contiguous(), [ra.RopeAxis(64)],
+                                torch.empty(9, 32, 2, device="cuda"))
+
+    def calls(x, w, q):
+        return [ra.rapid_linear(x, w, torch.empty(2, 9, 40, dtype=x.dtype, device="cuda")), ra.rapid_norm_modulate(x, torch.empty_like(x)),
+                *ra.rapid_qk_norm_rope([(q[0], q[1], torch.empty_like(q[0]), torch.empty_like(q[0]))], None, table),
+                *ra.rapid_rope([(q[0], q[1], torch.empty_like(q[0]), torch.empty_like(q[0]))], table)]
+
+    want = calls(x, w, q)
+    got = calls(*(t.clone().requires_grad_() for t in (x, w, q)))
+    for a, b in zip(got, want):
+        assert a.grad_fn is None and not a.requires_grad and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("value", [2.0 ** 64, -(2.0 ** 127)])
+def test_squares_that_leave_the_range_of_fp32(value):
+    """What the header says of such a row: zeros under the norm, and other rows as they are."""
+    x = normal((1, 5, 64), 1)
+    clean = ra.rapid_norm_modulate(x, torch.empty_like(x))
+    large = x.clone()
+    large[0, 2] = torch.tensor([value, -value], device="cuda").repeat(32)
+    got = ra.rapid_norm_modulate(large, torch.empty_like(x))
+    assert (got[0, 2] == 0).all() and torch.equal(got[0, [0, 1, 3, 4]], clean[0, [0, 1, 3, 4]])
+    q, k = ra.rapid_qk_norm_rope([(large[None], x[None], torch.empty_like(x[None]), torch.empty_like(x[None]))])
+    assert (q[0, 0, 2] == 0).all() and torch.isfinite(k).all() and torch.equal(q[0, 0, [0, 1, 3, 4]], k[0, 0, [0, 1, 3, 4]])
+
+
+def test_equal_rows_differ_by_the_order_of_a_sum_at_most():
+    """4096 times one row in tiles that begin at other steps: outputs within what two fp32 sums of K terms (each off by K roundings of
+    the absolute sum) and the rounding of each to bf16 can be apart."""
+    K, N = 1536, 4608
+    x, w = normal((1, K), 1).expand(4096, K).contiguous(), normal((N, K), 2, K ** -0.5)
+    y = widen(ra.rapid_linear(x, w, torch.empty(4096, N, dtype=x.dtype, device="cuda")))
+    sums = np.abs(widen(x[:1])) @ np.abs(widen(w)).T
+    assert (y.max(0) - y.min(0) <= 2 * (K * 2.0 ** -23 * sums[0]) * (1 + BF16_STEP) + 2 * BF16_STEP * np.abs(y).max(0)).all()
