@@ -593,6 +593,12 @@ def _check_layer(status: int):
         raise RapidAttnError(status, _LAYER_ERRORS.get(status, "unknown status"))
 
 
+def _ints(*sizes):
+    """Sizes that the entry points take as 32-bit integers (ctypes keeps the low bits of larger ones and says nothing)"""
+    if any(not -(1 << 31) <= n < 1 << 31 for n in sizes):
+        _check_layer(STATUS["RAPID_ERR_SHAPE"])
+
+
 def _on_device(device, call):
     """call(stream) with torch's current stream of `device`, which is made the current device meanwhile (the default stream's
     handle names none)."""
@@ -612,6 +618,7 @@ def _rows(name, t, device=None):
     if device is not None and t.get_device() != device:
         raise ValueError(f"{name} is on another device")
     B, (n, width) = (t.shape[0] if t.dim() == 3 else 1), t.shape[-2:]
+    _ints(B, n, width)
     return Rows(t.data_ptr(), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)), B, n, width
 
 
@@ -629,6 +636,8 @@ def _vectors(name, t, B, width, device):
 
 
 def rapid_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    if max(M, N, K) >= 1 << 31:                            # (not valid; of longer ones ctypes keeps the low bits)
+        return 0
     return int(library().rapid_linear_workspace_bytes(M, N, K))
 
 
@@ -750,6 +759,7 @@ def _qk_rows(segments, weights, table, layout):
         if k.stride() != q.stride() or k_out.stride() != q_out.stride():
             raise ValueError(f"segment {i}: q and k, and q_out and k_out, must share their strides")
         B, H, n, D = q.shape
+        _ints(B, H, n, D)
         first = first or (B, H, D)
         if (B, H, D) != first:
             raise ValueError("segments differ in B, H or D")

@@ -120,3 +120,24 @@ def test_equal_rows_differ_by_the_order_of_a_sum_at_most():
     y = widen(ra.rapid_linear(x, w, torch.empty(4096, N, dtype=x.dtype, device="cuda")))
     sums = np.abs(widen(x[:1])) @ np.abs(widen(w)).T
     assert (y.max(0) - y.min(0) <= 2 * (K * 2.0 ** -23 * sums[0]) * (1 + BF16_STEP) + 2 * BF16_STEP * np.abs(y).max(0)).all()
+
+
+FAR = (1 << 32) + 1                                        # 1 in its low 32 bits
+
+
+def test_sizes_beyond_32_bits(form):
+    """(one element for each row, so that nothing is allocated)"""
+    x, w = normal((1, 64), 1), normal((40, 64), 2)
+    y, q = torch.empty(1, 40, dtype=x.dtype, device="cuda"), normal((1, 1, 1, 64), 3)
+    table = torch.zeros(1, 32, 2, device="cuda")
+    far = q.expand(FAR, 1, 1, 64), q.expand(1, FAR, 1, 64), q.expand(1, 1, FAR, 64)
+    kept = [t.clone() for t in (x, y, q)]
+    calls = [lambda: ra.rapid_linear(x.expand(FAR, 64), w, y.expand(FAR, 40)), lambda: ra.rapid_linear(x.expand(FAR, 1, 64), w, y.expand(FAR, 1, 40)),
+             lambda: ra.rapid_norm_modulate(x.expand(FAR, 64), x.expand(FAR, 64)), lambda: ra.rapid_norm_modulate(x.expand(FAR, 1, 64), x.expand(FAR, 1, 64))]
+    calls += [lambda t=t: ra.rapid_qk_norm_rope([(t, q.clone().expand(t.shape), t, q.clone().expand(t.shape))]) for t in far]
+    calls += [lambda t=t: ra.rapid_rope([(t, q.clone().expand(t.shape), t, q.clone().expand(t.shape))], table) for t in far[:2]]
+    for call in calls:
+        with pytest.raises(ra.RapidAttnError) as e:
+            call()
+        assert e.value.status == ra.STATUS["RAPID_ERR_SHAPE"]
+    assert all(torch.equal(a, b) for a, b in zip((x, y, q), kept))

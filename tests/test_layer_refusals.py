@@ -48,3 +48,10 @@ def test_outputs_that_begin_where_a_tensor_of_the_other_segment_does(which, name
     other = dict(q=11 * A, k=12 * A, q_out=13 * A, k_out=14 * A)
     segs = ({}, {**other, name: at * A})
     assert qk(segs=segs[::-1] if which else segs, norm=norm) == ALIAS
+
+
+def test_workspaces_of_sizes_beyond_32_bits():
+    import paper_2509_22323_amd as ra
+    assert ra.rapid_linear_workspace_bytes(300, 320, 4096) > 0
+    for size in ((300 + (1 << 32), 320, 4096), (300, 320 + (1 << 32), 4096), (300, 320, 4096 + (1 << 32)), (300, 320, 4096 + (1 << 31))):
+        assert ra.rapid_linear_workspace_bytes(*size) == 0
