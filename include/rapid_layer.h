@@ -35,7 +35,7 @@ extern "C" {
 /*
  * The rows of a [B, n, width] tensor: row r of sample b starts at ptr + b*stride_b + r*stride_n (elements), its elements are
  * contiguous.  A slice of a joint [B, N, width] tensor is one (stride_b = N*width).
- *   constraints  0 <= stride_b, stride_n <= 2^22 elements; strides of dimensions of size 1 (stride_b when B == 1, stride_n
+ *   constraints  0 <= stride_b <= 2^40, 0 <= stride_n <= 2^22 elements; strides of dimensions of size 1 (stride_b when B == 1, stride_n
  *                when n == 1) address nothing and are not looked at.  Where rows are written no two may share an element.
  */
 typedef struct rapid_rows {

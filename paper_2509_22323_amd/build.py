@@ -27,7 +27,7 @@ FLAGS = [
     # no HIP runtime is linked in: the library binds to the libamdhip64 already loaded
     # in the process (PyTorch's), so streams and pointers belong to the same runtime
     "-no-hip-rt",
-    # packed fp32 VALU forms are kept off on the test machines
+    # packed fp32 VALU forms are kept off: some of them have given wrong results now and then
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
     "-I", os.path.join(ROOT, "include"),

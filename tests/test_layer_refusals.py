@@ -55,3 +55,17 @@ def test_workspaces_of_sizes_beyond_32_bits():
     assert ra.rapid_linear_workspace_bytes(300, 320, 4096) > 0
     for size in ((300 + (1 << 32), 320, 4096), (300, 320 + (1 << 32), 4096), (300, 320, 4096 + (1 << 32)), (300, 320, 4096 + (1 << 31))):
         assert ra.rapid_linear_workspace_bytes(*size) == 0
+
+
+def test_strides_at_their_limits():
+    """Of a row 2^22, of a sample and of its vectors 2^40; calls within them are refused for their alignment, behind this check."""
+    wide = dict(B=2, x=(A, 256, 64), y=(3 * A, 128, 32))
+    assert linear(**{**wide, "y": (3 * A + 1, 1 << 40, 1 << 22)}) == ALIGN
+    assert linear(**{**wide, "y": (3 * A + 1, (1 << 40) + 1, 32)}) == SHAPE and linear(**{**wide, "y": (3 * A + 1, 1 << 40, (1 << 22) + 1)}) == SHAPE
+    assert linear(**wide, res=(A + 1, 1 << 40, 0)) == ALIGN and linear(**wide, res=(A + 1, (1 << 40) + 1, 0)) == SHAPE
+    assert linear(**wide, gate=A + 1, gs=1 << 40) == ALIGN and linear(**wide, gate=A + 1, gs=(1 << 40) + 1) == SHAPE
+    rows = dict(B=2, x=(A + 2, 1 << 40, 1 << 22), y=(3 * A, 1 << 40, 1 << 22), ss=1 << 40, hs=1 << 40)
+    assert modulate(**rows) == ALIGN
+    for far in (dict(x=(A + 2, (1 << 40) + 8, 64)), dict(x=(A + 2, 256, (1 << 22) + 8)), dict(y=(3 * A, (1 << 40) + 8, 64)), dict(ss=(1 << 40) + 8),
+                dict(hs=(1 << 40) + 8)):
+        assert modulate(**{**rows, **far}) == SHAPE
