@@ -185,9 +185,10 @@ __device__ __forceinline__ bf16x8 finished(const LinearParams& p, float (&z)[8],
 // row side by side.  Copies go from memory into LDS past the registers, two or three steps ahead, one barrier a step; workgroups
 // stay and go on to their next item, whose first steps are on their way before the results of the last one are written.
 //
-// Bound by the matrix pipe and the clock it leaves: 8192 rows, 9728 -> 2432 (388 GFLOP, tile 256 x 160) takes 291 us = 1.33 PFLOP/s, the
-// pipe busy 72 % of the cycles; the same loop without copies 264, without reads of LDS 250, without either 234, without the barrier 285.
-// 8192 rows, 1536 -> 4608 (116 GFLOP, 256 x 192): 99 us, of which the ends of tiles are a sixth.  Measured and not taken: other
+// Bound by the matrix pipe and the clock it leaves: 8192 rows, 9728 -> 2432 (388 GFLOP, tile 256 x 160) takes 291 to 320 us from card to
+// card (1.33 to 1.21 PFLOP/s), the pipe busy 70 to 72 % of the cycles; on the card where it takes 291 the same loop takes 264 without
+// copies, 250 without reads of LDS, 234 without either, 285 without the barrier.
+// 8192 rows, 1536 -> 4608 (116 GFLOP, 256 x 192): 98 to 104 us, of which the ends of tiles are a sixth.  Measured and not taken: other
 // orders of tiles (GROUP 2, 6, 8, 16), weights past the caches, touching the next steps in the L2 first, 128 x 64 outputs a wavefront
 // with four wavefronts, all copies in a step's first half, priorities of waves, five steps in LDS for the small tiles: none faster over
 // products of 64 to 8192 rows, most 1 to 20 % slower.
@@ -761,8 +762,9 @@ struct Plan {
 // counts more than the mean); every round has `ends` (`odd` more where the width is no multiple of eight), every call `call`.
 // Pieces are added up by a second kernel, which costs `join` and `sum` for every million numbers that it reads.  Fitted to 1050
 // products of 9 to 32768 rows, 16 to 9728 outputs and 64 to 9728 inputs (odd sizes among them), timed in all tiles and 1 to 8
-// pieces, inputs changing from call to call: the plan found by it takes 1.010 times what the best one does in the geometric mean
-// (1.33 times at most).
+// pieces, inputs changing from call to call: the plan found by it takes 1.01 times what the best one does in the geometric mean.  So it
+// does for 700 others of these ranges (1.4 times at most) and for 100 of up to 21504 outputs or inputs (1.15 at most), whose times in
+// every form are in profiles/linear_tiles.txt.
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;

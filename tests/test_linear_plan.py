@@ -1,9 +1,13 @@
 """The host's choice of a product's kernel: what the products of the GPU tests are taken in (so that other costs cannot silently leave a
 tile untested), and its rules at the ends of their ranges.  No GPU needed."""
+import math
+import os
+
 import pytest
 
 import linear_plan
 import paper_2509_22323_amd as ra
+from paper_2509_22323_amd import build
 
 
 @pytest.fixture(scope="module")
@@ -38,3 +42,25 @@ def test_workspaces_are_those_of_the_plan(plan):
 def test_any_size_has_a_plan(plan, M, N, K):
     tile, pieces = plan(M, N, K)
     assert tile == "dots" and M <= 8 or 1 <= pieces <= 8 and (pieces == 1 or 3 * pieces * 64 <= K and M * N < 1 << 31)
+
+
+def timed():
+    """(rows, outputs, inputs, us of the library, us of each form) of the products that were timed in every form"""
+    path = os.path.join(os.path.dirname(build.HERE), "profiles", "linear_tiles.txt")
+    forms = [(t, p) for t in linear_plan.TILES[:2] for p in range(1, 9)] + [(t, 1) for t in linear_plan.TILES[2:]]
+    for line in open(path):
+        if line[0].isdigit():
+            m, n, k, library, *times = line.split()
+            yield int(m), int(n), int(k), float(library), {f: float(t) for f, t in zip(forms, times, strict=True) if t != "-"}
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_the_plan_costs_little_over_the_best_form(plan, wide):
+    """In the times that are committed beside the costs: 1.01 in the geometric mean, of products within the fit's range and beyond it, and
+    no more than the comment on the costs says."""
+    over = []
+    for m, n, k, _, times in timed():
+        if (max(n, k) > 9728) == wide:
+            over.append(times[plan(m, n, k)] / min(times.values()))
+    assert len(over) == (100 if wide else 700)
+    assert math.exp(sum(map(math.log, over)) / len(over)) <= 1.015 and max(over) <= (1.15 if wide else 1.4)
