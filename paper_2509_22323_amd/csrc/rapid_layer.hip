@@ -164,8 +164,10 @@ struct QkParams {
 // Heads of a lane group: 4 rows (queries and keys) in flight.  One head: 34 us at 4608 tokens of 24 heads of 128, two 29.5, four
 // 30.5 (fewer workgroups, the last of them alone); small calls are faster the more workgroups there are.  Loads past the caches
 // would gain 6 % where the rows come from memory and cost 20 % where the projection has just left them in the caches.  28 us at 4608
-// tokens of 24 heads of 128 in a fused projection (115 MB, 4.1 TB/s; 22.6 from the caches), 87 us at 16896 head after head (424 MB,
-// 4.9 TB/s; the table is fetched once a part, 80 MB more: workgroups in an order that keeps its rows in one L2 took 94).
+// tokens of 24 heads of 128 in a fused projection (115 MB, 4.1 TB/s; 22.6 from the caches), 88 us at 16896 head after head (424 MB,
+// 4.8 TB/s; the table is fetched once a part, 80 MB more: workgroups in an order that keeps its rows in one L2 took 94).
+// In halves 4 to 9 % more (eight angles a lane, four moves between lanes for 16 bytes, six wavefronts a SIMD for eight): 31.7 us for 29.3 at
+// the first size, 99.6 for 92.4 at the second with the norm, 89.7 for 85.6 without.
 constexpr int HEADS = 2;
 
 // A group of D / 8 lanes takes one token: its row of the table, and heads part, part + parts, .. of queries and keys.

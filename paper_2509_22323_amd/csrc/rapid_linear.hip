@@ -641,7 +641,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
 // ---------------------------------------------------------------------------
 // A handful of rows (the conditioning's projections): MAX_M of x at most.  A wavefront takes OUT outputs of all rows and reads their
 // rows of w end to end, 1 KB an access; two products an instruction, the lanes' sums are added at the end.  Bound by the bytes of w:
-// 2 rows, 1536 -> 9216 (28 MB): 4.7 us = 6.0 TB/s where w is in the caches, 6.9 us = 4.1 TB/s where w changes
+// 2 rows, 1536 -> 9216 (28 MB): 4.7 us = 6.0 TB/s where w is in the caches, 6.6 us = 4.3 TB/s where w changes
 // from call to call; four outputs a wavefront and four wavefronts a workgroup, whose number then does not go evenly over the CUs:
 // 4.9 and 7.2, and 9.2 instead of 5.3 us for 4 rows, 9728 -> 100.
 // ---------------------------------------------------------------------------
@@ -712,8 +712,8 @@ __global__ __launch_bounds__(DOT_WAVES * 64) void linear_dot_kernel(LinearParams
     p.y[b * p.y_sb + (long long)r * p.y_sn + n] = (__bf16)mine;
 }
 
-// Every wavefront reads all of x.  Five to eight rows: 9.9 us here, 11.6 in tiles of matrix instructions at 1536 -> 9216, 8.8 / 11.6 at
-// 6144 -> 1536, but 20.5 / 16.7 at 2432 -> 14592.
+// Every wavefront reads all of x.  Five to eight rows, three sets of inputs in turn: 10.6 to 11.0 us here, 11.5 in tiles of matrix
+// instructions at 1536 -> 9216, 8.9 to 9.2 and 11.5 at 6144 -> 1536, but 21 and 16.7 at 2432 -> 14592.  (Four: 7.7, 6.9 and 14.2 here.)
 bool by_dots(long long M, int N, int K) { return M <= 4 || (M <= 8 && (long long)N * K <= 1 << 24); }
 
 // Rows of y, residual and gate that start at multiples of four bytes, or results too small for it to matter: 8192 rows, 1536 -> 4607 with
