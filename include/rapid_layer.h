@@ -116,7 +116,8 @@ typedef struct rapid_rope_axis {
 
 /*
  * table[t, i, :] = magnitude * (cos a, sin a), a = positions[t, axis of i] * f_i; the pairs of axis 0 come first.
- * Angles are reduced in fp64: an entry is off by half a step of fp32 and |magnitude| (2^-29 + 2^-52 |a|) at most.
+ * Angles are reduced in fp64: an entry is off by half a step of fp32 and |magnitude| (2^-29 + 2^-52 |a|) at most, and by what the
+ * blend of a scaling by parts, taken in fp64, is off.
  *   positions  device, int32 [tokens, n_axes], any value, 4-byte aligned
  *   axes       HOST array of n_axes (1 .. 8) descriptors; the dims add up to rot, a multiple of 16 up to 128
  *   table      device, fp32 [tokens, rot/2, 2], 16-byte aligned
