@@ -41,6 +41,8 @@ MASK_EXPORTS = ("rapid_mask_select", "rapid_mask_select_workspace_bytes", "rapid
                 "rapid_attn_joint_select_workspace_bytes", "rapid_mask_level_tau")
 LAYER_EXPORTS = ("rapid_linear", "rapid_linear_workspace_bytes", "rapid_norm_modulate", "rapid_rope_table", "rapid_qk_norm_rope",
                  "rapid_rope")
+PACKED_EXPORTS = ("rapid_quantize_rows", "rapid_norm_modulate_int8", "rapid_linear_int8", "rapid_linear_int8_workspace_bytes",
+                  "rapid_attn_packed", "rapid_attn_packed_workspace_bytes")
 CACHE_EXPORTS = ("rapid_cache_store", "rapid_cache_reuse", "rapid_equivalent_steps", "rapid_reward")
 
 
@@ -159,6 +161,18 @@ def library():
     lib.rapid_qk_norm_rope.restype = ci
     lib.rapid_rope.argtypes = [ctypes.POINTER(QkSegment), ci, ci, ci, ci, vp, ll, ci, ci, vp]
     lib.rapid_rope.restype = ci
+    lib.rapid_quantize_rows.argtypes = [rows, rows, vp, ci, ci, ci, vp]
+    lib.rapid_quantize_rows.restype = ci
+    lib.rapid_norm_modulate_int8.argtypes = [rows, rows, vp, vp, ll, vp, ll, vp, ci, ci, ci, ci, cf, vp]
+    lib.rapid_norm_modulate_int8.restype = ci
+    lib.rapid_linear_int8.argtypes = [rows, vp, vp, ll, vp, vp, rows, ci, vp, ll, rows, vp, ci, ci, ci, ci, ci, vp, sz, vp]
+    lib.rapid_linear_int8.restype = ci
+    lib.rapid_linear_int8_workspace_bytes.argtypes = [ll, ci, ci]
+    lib.rapid_linear_int8_workspace_bytes.restype = sz
+    lib.rapid_attn_packed.argtypes = [ctypes.POINTER(Segment), ci, ci, ci, ci, vp, ll, vp, ll, cf, cf, vp, sz, vp]
+    lib.rapid_attn_packed.restype = ci
+    lib.rapid_attn_packed_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.rapid_attn_packed_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -609,12 +623,12 @@ def _on_device(device, call):
         return call(torch._C._cuda_getCurrentRawStream(device))
 
 
-def _rows(name, t, device=None):
+def _rows(name, t, device=None, dtype="bfloat16"):
     """(descriptor, B, n, width) of a bf16 tensor [B, n, width], or [n, width] (B = 1), with a contiguous last dimension"""
     import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() in (2, 3)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is getattr(torch, dtype) and t.dim() in (2, 3)
             and (t.stride(-1) == 1 or t.shape[-1] == 1)):
-        raise TypeError(f"{name} must be a CUDA bfloat16 tensor [B,n,width] or [n,width] with a contiguous last dimension")
+        raise TypeError(f"{name} must be a CUDA {dtype} tensor [B,n,width] or [n,width] with a contiguous last dimension")
     if device is not None and t.get_device() != device:
         raise ValueError(f"{name} is on another device")
     B, (n, width) = (t.shape[0] if t.dim() == 3 else 1), t.shape[-2:]
@@ -817,3 +831,180 @@ def rapid_rope(segments, table, layout="interleaved"):
     _check_layer(_on_device(device, lambda stream: library().rapid_rope(
         descr, len(segments), B, H, D, table_ptr, table_stride, rot, lay, stream)))
     return [t for seg in segments for t in seg[2:]]
+
+
+# ---------------------------------------------------------------- layers in 8 bits over packed sequences
+# Operators of inference, as those above: not recorded by autograd, no gradients.
+_PACKED_ERRORS = {
+    **_LAYER_ERRORS,
+    -3: "unsupported: widths of rows are multiples of 8 (inputs of a product of 16, at most 2^17 - 16; a norm's 16384 at most), heads 64 "
+        "or 128 wide, a cap finite and not negative; see include/rapid_packed.h",
+    -4: "a pointer or stride is not aligned (bf16 16 bytes and 8 elements, 8-bit rows 8 bytes, of a product 16; outputs, biases and gates of a product 2 bytes)",
+}
+_ANY_DOCUMENT = (1 << 31) - 1
+
+
+def _check_packed(status: int):
+    if status != 0:
+        raise RapidAttnError(status, _PACKED_ERRORS.get(status, "unknown status"))
+
+
+def _per_row(name, t, dtype, B, n, device):
+    """Pointer of a contiguous tensor [B, n], or [n] where B is 1; None"""
+    import torch
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is getattr(torch, dtype) and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous CUDA {dtype} tensor [B,n]")
+    if tuple(t.shape) not in (((B, n), (n,)) if B == 1 else ((B, n),)) or t.get_device() != device:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != {(B, n)}, or another device")
+    return t.data_ptr()
+
+
+def _document_vectors(vectors, document, B, width, device):
+    """((pointer, stride) of each, their number) of the conditioning's vectors {name: tensor or None}: [B, width] or [width], or, with
+    document, [documents, width] or [width]"""
+    if document is None:
+        return [_vectors(name, t, B, width, device) for name, t in vectors.items()], 0
+    counts = {t.shape[0] for t in vectors.values() if t is not None and getattr(t, "ndim", 1) == 2}
+    if len(counts) > 1:
+        raise ValueError(f"{' and '.join(vectors)}: vectors of as many documents, not of {sorted(counts)}")
+    documents = counts.pop() if counts else _ANY_DOCUMENT
+    _ints(documents)
+    return [_vectors(name, t, documents, width, device) for name, t in vectors.items()], documents
+
+
+def rapid_quantize_rows(x, q, scale):
+    """q, scale <- the rows of x as 8-bit integers: q = round(127 x / m), ties to even, scale = m / 127, m the row's largest magnitude.
+    x: CUDA bf16 [B,n,K] (or [n,K]), q: int8 of its shape, last dimensions contiguous; scale: float32 [B,n] (or [n]) contiguous.
+    Weights are quantised by the same call.  Inference only: not recorded by autograd, no gradients.  Returns (q, scale)."""
+    xr, B, n, K = _rows("x", x)
+    device = x.get_device()
+    qr, *shape = _rows("q", q, device, "int8")
+    if shape != [B, n, K]:
+        raise ValueError(f"q: {tuple(q.shape)} does not go with x: {tuple(x.shape)}")
+    if scale is None:
+        raise TypeError("scale must be a contiguous CUDA float32 tensor [B,n]")
+    scale_ptr = _per_row("scale", scale, "float32", B, n, device)
+    _check_packed(_on_device(device, lambda stream: library().rapid_quantize_rows(xr, qr, scale_ptr, B, n, K, stream)))
+    return q, scale
+
+
+def rapid_norm_modulate_int8(x, q, q_scale, scale=None, shift=None, eps=1e-6, document=None):
+    """q, q_scale <- as rapid_quantize_rows of (x - mean) / sqrt(variance + eps) * (1 + scale) + shift, which is not rounded in between.
+    x, q, q_scale as there; scale, shift: CUDA bf16 [B,C] or [C], both or neither; with document (int32 [B,n], or [n], contiguous)
+    they are [documents,C], numbered by it, and rows of no document (-1) are left as they were.
+    Inference only: not recorded by autograd, no gradients.  Returns (q, q_scale)."""
+    xr, B, n, C = _rows("x", x)
+    device = x.get_device()
+    qr, *shape = _rows("q", q, device, "int8")
+    if shape != [B, n, C]:
+        raise ValueError(f"q: {tuple(q.shape)} does not go with x: {tuple(x.shape)}")
+    if (scale is None) != (shift is None):
+        raise ValueError("scale and shift: both or neither")
+    if q_scale is None:
+        raise TypeError("q_scale must be a contiguous CUDA float32 tensor [B,n]")
+    q_scale_ptr = _per_row("q_scale", q_scale, "float32", B, n, device)
+    document_ptr = _per_row("document", document, "int32", B, n, device)
+    ((scale_ptr, scale_stride), (shift_ptr, shift_stride)), documents = _document_vectors(
+        dict(scale=scale, shift=shift), document, B, C, device)
+    _check_packed(_on_device(device, lambda stream: library().rapid_norm_modulate_int8(
+        xr, qr, q_scale_ptr, scale_ptr, scale_stride, shift_ptr, shift_stride, document_ptr, documents, B, n, C, float(eps), stream)))
+    return q, q_scale
+
+
+def rapid_linear_int8_workspace_bytes(M: int, N: int, K: int) -> int:
+    if max(M, N, K) >= 1 << 31:                            # (not valid; of longer ones ctypes keeps the low bits)
+        return 0
+    return int(library().rapid_linear_int8_workspace_bytes(M, N, K))
+
+
+def rapid_linear_int8(x, x_scale, weight, w_scale, out, bias=None, activation="none", gate=None, residual=None, document=None,
+                      workspace=None):
+    """out <- residual + gate * act(x_scale w_scale (x weight^T) + bias).  x: CUDA int8 [B,n,K] (or [n,K]) with x_scale float32
+    [B,n] (or [n]), weight: int8 [N,K] with w_scale float32 [N], as rapid_quantize_rows makes them; out, bias, activation, gate and
+    residual as rapid_linear.  With document (int32 [B,n], or [n], contiguous) gate is [documents,N] (or [N]), numbered by it, and rows
+    of no document (-1) are left as they were.  `workspace`: CUDA uint8 tensor of at least rapid_linear_int8_workspace_bytes(B*n, N, K)
+    bytes; allocated with torch if None.  The same row of x gives the same bits in whatever call.
+    Inference only: not recorded by autograd, no gradients.  Returns out."""
+    import torch
+    xr, B, n, K = _rows("x", x, None, "int8")
+    device = x.get_device()
+    outr, Bo, no, N = _rows("out", out, device)
+    if (Bo, no) != (B, n):
+        raise ValueError(f"out: {tuple(out.shape)} does not go with x: {tuple(x.shape)}")
+    if not (isinstance(weight, torch.Tensor) and weight.is_cuda and weight.dtype is torch.int8 and weight.dim() == 2
+            and (weight.stride(1) == 1 or K == 1)):
+        raise TypeError("weight must be a CUDA int8 tensor [N,K] with a contiguous last dimension")
+    if tuple(weight.shape) != (N, K) or weight.get_device() != device:
+        raise ValueError(f"weight: shape {tuple(weight.shape)} != {(N, K)}, or another device")
+    if x_scale is None or w_scale is None:
+        raise TypeError("x_scale and w_scale must be contiguous CUDA float32 tensors [B,n] and [N]")
+    x_scale_ptr = _per_row("x_scale", x_scale, "float32", B, n, device)
+    w_scale_ptr = _per_row("w_scale", w_scale, "float32", 1, N, device)
+    document_ptr = _per_row("document", document, "int32", B, n, device)
+    bias_ptr, _ = _vectors("bias", bias, 1, N, device)
+    ((gate_ptr, gate_stride),), documents = _document_vectors(dict(gate=gate), document, B, N, device)
+    res = None
+    if residual is not None:
+        res, Br, nr, Nr = _rows("residual", residual, device)
+        if (Br, nr, Nr) != (B, n, N):
+            raise ValueError(f"residual: {tuple(residual.shape)} does not go with out: {tuple(out.shape)}")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    if workspace is None:
+        need = rapid_linear_int8_workspace_bytes(B * n, N, K)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    elif not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()
+              and workspace.get_device() == device):
+        raise TypeError("workspace must be a contiguous CUDA tensor on x's device")
+    ws_ptr, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check_packed(_on_device(device, lambda stream: library().rapid_linear_int8(
+        xr, x_scale_ptr, weight.data_ptr(), weight.stride(0) if N > 1 else K, w_scale_ptr, bias_ptr, outr, ACTIVATIONS[activation],
+        gate_ptr, gate_stride, res, document_ptr, documents, B, n, N, K, ws_ptr, ws_bytes, stream)))
+    return out
+
+
+def rapid_attn_packed_workspace_bytes(B: int, H: int, N: int, D: int) -> int:
+    if max(B, H, N, D) >= 1 << 31:
+        return 0
+    return int(library().rapid_attn_packed_workspace_bytes(B, H, N, D))
+
+
+def _per_token(name, t, B, N, device):
+    """(pointer, stride of a sample) of an int32 tensor [B, N], or [N] (one for all samples), with a contiguous last dimension"""
+    import torch
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.int32 and t.dim() in (1, 2)
+            and (t.stride(-1) == 1 or t.shape[-1] == 1)):
+        raise TypeError(f"{name} must be a CUDA int32 tensor [B,N] or [N] with a contiguous last dimension")
+    if tuple(t.shape) not in ((B, N), (N,)) or t.get_device() != device:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != {(B, N)}, or another device")
+    return t.data_ptr(), t.stride(0) if t.dim() == 2 else 0
+
+
+def rapid_attn_packed(segments, document, order=None, cap=0.0, scale=0.0, workspace=None):
+    """Attention of documents packed into one joint sequence: token i takes part in token j's softmax where document[i] == document[j]
+    >= 0 and order[i] <= order[j] (order None: wherever the documents agree); tokens of no document (-1) output zeros.  `segments`:
+    one or two (q, k, v, o) as rapid_attn_joint takes them, of any lengths; document, order: CUDA int32 [B,N] or [N] over the joint
+    tokens; cap > 0: scores s become cap * tanh(s / cap).  `workspace`: CUDA uint8 tensor of at least
+    rapid_attn_packed_workspace_bytes(B, H, N, D) bytes; allocated with torch if None.
+    Inference only: not recorded by autograd, no gradients.  Returns the o tensors."""
+    import torch
+    descr, B, H, N, D = _segments(segments)
+    q0 = segments[0][0]
+    device = q0.get_device()
+    if any(seg[0].get_device() != device for seg in segments):
+        raise ValueError("segments are on different devices")
+    _ints(B, H, N, D)
+    document_ptr, document_stride = _per_token("document", document, B, N, device)
+    order_ptr, order_stride = (None, 0) if order is None else _per_token("order", order, B, N, device)
+    if workspace is None:
+        workspace = torch.empty(max(rapid_attn_packed_workspace_bytes(B, H, N, D), 16), dtype=torch.uint8, device=q0.device)
+    elif not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()
+              and workspace.get_device() == device):
+        raise TypeError("workspace must be a contiguous CUDA tensor on the segments' device")
+    _check_packed(_on_device(device, lambda stream: library().rapid_attn_packed(
+        descr, len(segments), B, H, D, document_ptr, document_stride, order_ptr, order_stride, float(cap), float(scale),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)))
+    return [seg[3] for seg in segments]
