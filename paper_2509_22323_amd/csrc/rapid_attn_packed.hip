@@ -1,5 +1,6 @@
 // Attention of documents packed into one joint sequence, for MI355X (gfx950).  C ABI: include/rapid_packed.h.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -10,6 +11,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.44269504088896340736f;
@@ -20,12 +22,15 @@ struct Side {                                          // of a segment
     long long in_sb, in_sh, out_sb, out_sh;            // bytes
     int in_sn, out_sn;                                 // bytes
 };
+struct Known;
 struct PackedParams {
     Side side[2];
     const int* document;
     const int* order;                                  // or null
     long long document_sb, order_sb;
     int n0, N, B, H;                                   // tokens of the first segment, of both
+    int tiles0, tiles, groups0, groups1;               // tiles of the first segment, of both; groups of 128 queries of each
+    Known* known;                                      // [B, tiles]
     float scale;                                       // of a score: capped / log2(e), else as exponent of 2
     float cap;                                         // as exponent of 2; 0: none
 };
@@ -48,7 +53,7 @@ __device__ __forceinline__ float exponent(float s, float scale, float cap)
 {
     if (cap == 0.f) return s * scale;
     // cap tanh(u) = cap - 2 cap / (1 + exp(2 u)), scale = 2 log2(e) scale' / cap'
-    return cap - 2.f * cap / (1.f + __builtin_amdgcn_exp2f(s * scale));
+    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * scale)), cap);
 }
 
 // One row of the output by one wavefront, key by key: a lane a key for the scores, D / 64 elements of the output a lane.
@@ -100,13 +105,353 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
     for (int c = 0; c < EACH; ++c) o[c] = (__bf16)(own >= 0 ? acc[c] / l : 0.f);
 }
 
-template <int D>
-__global__ __launch_bounds__(256) void attn_packed_simple_kernel(PackedParams p)
+// ---------------------------------------------------------------------------
+// Tiles of 64 tokens, counted within each segment (the last one of a segment may be short).  What is known of a tile:
+// ---------------------------------------------------------------------------
+constexpr int TILE = 64, ROWS = 128;                   // keys of a tile; queries of a workgroup
+constexpr int WAVES = ROWS / 32;
+
+struct Known {
+    int first, last;                                   // smallest (~ it: some token is of no document) and largest document; last < 0: none
+    int early, late;                                   // smallest and largest order
+};
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ int smallest(const Known& k) { return k.first < 0 ? ~k.first : k.first; }
+
+// Of tile `tile` of a sample, by a wavefront.
+__device__ __forceinline__ Known known_of(const PackedParams& p, int b, int tile, int lane)
 {
-    const long long rows = (long long)p.B * p.H * p.N;
-    for (long long row = blockIdx.x * 4LL + (threadIdx.x >> 6); row < rows; row += gridDim.x * 4LL) {
-        const int head = (int)(row / p.N);
-        row_by_keys<D>(p, head / p.H, head % p.H, (int)(row - (long long)head * p.N), threadIdx.x & 63);
+    const bool second = tile >= p.tiles0;
+    const int row = (second ? tile - p.tiles0 : tile) * TILE + lane, n = second ? p.N - p.n0 : p.n0;
+    const int t = min(row, n - 1) + (second ? p.n0 : 0);
+    const int d = p.document[b * p.document_sb + t], o = p.order ? p.order[b * p.order_sb + t] : 0;
+    const bool there = row < n && d >= 0;
+    Known k = {there ? d : INT_MAX, there ? d : -1, there ? o : INT_MAX, there ? o : INT_MIN};
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+        k.first = min(k.first, __shfl_xor(k.first, x, 64));
+        k.last = max(k.last, __shfl_xor(k.last, x, 64));
+        k.early = min(k.early, __shfl_xor(k.early, x, 64));
+        k.late = max(k.late, __shfl_xor(k.late, x, 64));
+    }
+    if (__builtin_amdgcn_ballot_w64(!there) != 0ull) k.first = ~k.first;
+    return k;
+}
+
+enum { NONE, SOME, ALL };
+// Whether queries of what is known as q see keys of k.
+__device__ __forceinline__ int sees(const Known& q, const Known& k)
+{
+    const int qf = smallest(q), kf = smallest(k);
+    if (q.last < 0 || k.last < 0 || kf > q.last || k.last < qf || k.early > q.late) return NONE;
+    return k.first == k.last && qf == q.last && k.first == qf && k.late <= q.early ? ALL : SOME;
+}
+
+// What is known of all tiles, a wavefront each.
+__global__ __launch_bounds__(256) void packed_known_kernel(PackedParams p)
+{
+    const int lane = threadIdx.x & 63, tile = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (tile >= p.tiles) return;
+    const Known k = known_of(p, blockIdx.y, tile, lane);
+    if (lane == 0) p.known[(long long)blockIdx.y * p.tiles + tile] = k;
+}
+
+// ---------------------------------------------------------------------------
+// The kernel: a workgroup takes 128 queries of a head, a wavefront 32 of them, and goes over the tiles that one of them sees.
+// S^T = K Q^T, one query a lane, and O^T += V^T P^T, v_mfma_f32_16x16x32_bf16; P goes from one product to the next in registers.
+// ---------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) char lds_char;
+
+template <int D>
+struct Lds {
+    static constexpr int RB = D * 2, BYTES = TILE * RB, COPIES = BYTES / 1024 / WAVES, PER = 1024 / RB;     // PER: rows of a copy
+    // 16-byte chunks of a row change places by row, so that the 16 rows (K) or 4 x 16 patches (V) that are read at a time lie in different banks
+    static __device__ __forceinline__ int turn_k(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
+    static __device__ __forceinline__ int turn_v(int row) { return D == 128 ? (row & 7) << 1 : (row >> 1 & 3) << 1; }
+};
+
+// 1 KB from 64 lanes' offsets into LDS; 5 wait states behind a vector instruction that wrote the descriptor, one behind the write of M0
+template <bool FIRST>
+__device__ __forceinline__ void copy_1k(const i32x4& buffer, unsigned off, unsigned dst)
+{
+    if constexpr (FIRST) asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(buffer));
+    else asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(buffer));
+}
+
+// Everything that this wavefront has requested has arrived, then the barrier; nothing moves across.
+__device__ __forceinline__ void arrive()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int D, bool CAP>
+__global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams p)
+{
+    typedef Lds<D> L;
+    constexpr int KS = D / 32, DT = D / 16;
+    constexpr int LIST = 1024;                         // tiles that are listed at a time
+    __shared__ __align__(1024) char lds[4 * L::BYTES];
+    __shared__ int list[LIST + 1];
+    __shared__ int found[WAVES + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+
+    // which rows
+    const int per = p.groups0 + p.groups1;
+    const unsigned items = (unsigned)(p.B * p.H) * per, each = items / 8, more = items % 8, x = blockIdx.x % 8;
+    const unsigned item = x * each + min(x, more) + blockIdx.x / 8;
+    const int head = __builtin_amdgcn_readfirstlane(item / per), b = __builtin_amdgcn_readfirstlane(head / p.H), h = head - b * p.H;
+    const int group = per - 1 - (int)(item - (unsigned)head * per);
+    const bool second = group >= p.groups0;
+    const Side& own = p.side[second];
+    const int length = second ? p.N - p.n0 : p.n0, row0 = (second ? group - p.groups0 : group) * ROWS;
+    const Known* known = p.known + (long long)b * p.tiles;
+    const int tile0 = (second ? p.tiles0 : 0) + row0 / TILE;
+    Known mine = known[tile0];
+    if (row0 + TILE < length) {
+        const Known k = known[tile0 + 1];
+        mine.first = min(smallest(mine), smallest(k));
+        mine.last = max(mine.last, k.last);
+        mine.early = min(mine.early, k.early);
+        mine.late = max(mine.late, k.late);
+    }
+
+    // queries: lane (n, g) holds elements 32 t + 8 g .. + 7 of query 16 q + n
+    const int q0 = row0 + 32 * wave;
+    bf16x8 qf[2][KS];
+    int doc[2], turn[2];
+    const long long at_in = b * own.in_sb + h * own.in_sh;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int row = min(q0 + 16 * q + n, length - 1), t = row + (second ? p.n0 : 0);
+        const char* from = own.q + at_in + (long long)row * own.in_sn + 16 * g;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[q][k] = *(const bf16x8*)(from + 64 * k);
+        doc[q] = p.document[b * p.document_sb + t];
+        turn[q] = p.order ? p.order[b * p.order_sb + t] : 0;
+    }
+
+    // copies of a tile: this lane's rows and chunks
+    const unsigned lds_at = (unsigned)(size_t)(lds_char*)lds;
+    const int crow = wave * L::COPIES * L::PER + lane / (64 / L::PER);
+    unsigned ck[L::COPIES], cv[L::COPIES];
+#pragma unroll
+    for (int j = 0; j < L::COPIES; ++j) {
+        const int row = crow + j * L::PER, c = lane % (64 / L::PER);
+        ck[j] = 16u * (c ^ L::turn_k(row));
+        cv[j] = 16u * (c ^ L::turn_v(row));
+    }
+    auto copy = [&](int entry, bool is_v, int slot) {
+        const int tile = entry & 0x3fffffff;
+        const bool s = tile >= p.tiles0;
+        const Side& from = p.side[s];
+        const int row = (s ? tile - p.tiles0 : tile) * TILE, rows = min((s ? p.N - p.n0 : p.n0) - row, TILE);
+        const unsigned long long base = (unsigned long long)((is_v ? from.v : from.k) + b * from.in_sb + h * from.in_sh + (long long)row * from.in_sn);
+        const i32x4 buffer = {(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), (rows - 1) * from.in_sn + L::RB, 0x00020000};
+        const unsigned at = crow * from.in_sn;
+#pragma unroll
+        for (int j = 0; j < L::COPIES; ++j) {
+            const unsigned off = at + (unsigned)(j * L::PER) * from.in_sn + (is_v ? cv[j] : ck[j]);
+            const unsigned dst = lds_at + slot * L::BYTES + (wave * L::COPIES + j) * 1024;
+            if (j == 0) copy_1k<true>(buffer, off, dst);
+            else copy_1k<false>(buffer, off, dst);
+        }
+    };
+
+    // fragments in a tile
+    unsigned kat[KS], vat[DT];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kat[k] = n * L::RB + (((4 * k + g) ^ L::turn_k(n)) << 4);
+    const int vrow = 4 * g + (n >> 2);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vat[d] = vrow * L::RB + (((2 * d + ((n & 3) >> 1)) ^ L::turn_v(vrow)) << 4) + (n & 1) * 8;
+
+    f32x4 acc[DT][2] = {}, sums[2] = {};
+    float m[2] = {-1e30f, -1e30f};
+    bool partly = false;
+    bf16x8 ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
+
+    typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+    auto scores = [&](int slot, f32x4 (&s)[4][2]) {
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const bf16x8 kf = *(lds_bf16x8*)((lds_char*)lds + slot * L::BYTES + kt * 16 * L::RB + kat[k]);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+                    s[kt][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[q][k], k == 0 ? none : s[kt][q], 0, 0, 0);
+                }
+            }
+        }
+    };
+    auto mask = [&](int entry, f32x4 (&s)[4][2]) {
+        const int tile = entry & 0x3fffffff;
+        const bool second = tile >= p.tiles0;
+        const int row = (second ? tile - p.tiles0 : tile) * TILE, rows = (second ? p.N - p.n0 : p.n0) - row;
+        const int* document = p.document + b * p.document_sb + (second ? p.n0 : 0) + row;
+        const int* order = p.order ? p.order + b * p.order_sb + (second ? p.n0 : 0) + row : nullptr;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int key = 16 * kt + 4 * g + r, at = min(key, rows - 1);
+                const int d = document[at], o = order ? order[at] : 0;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) s[kt][q][r] = key < rows && d == doc[q] && o <= turn[q] ? s[kt][q][r] : -INFINITY;
+            }
+    };
+    const float scale = p.scale, cap = p.cap;
+
+    const int tiles = p.tiles;
+    for (int from = 0; from < tiles; from += LIST) {
+        // the tiles that someone here sees, in order
+        const int upto = min(tiles - from, LIST);
+        int count = 0;
+        for (int i = 0; i < upto; i += WAVES * 64) {
+            const int tile = from + i + tid;
+            const int how = i + tid < upto ? sees(mine, known[tile]) : NONE;
+            const unsigned long long some = __builtin_amdgcn_ballot_w64(how != NONE);
+            __syncthreads();
+            if (lane == 0) found[wave] = __popcll(some);
+            __syncthreads();
+            int before = count;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) before += found[w];
+                count += found[w];
+            }
+            if (how != NONE) list[before + __popcll(some & ((1ull << lane) - 1ull))] = tile | (how == SOME ? 1 << 30 : 0);
+        }
+        __syncthreads();
+        count = __builtin_amdgcn_readfirstlane(count);
+        if (count == 0) continue;
+        auto entry = [&](int i) { return __builtin_amdgcn_readfirstlane(list[i]); };
+
+        // K: slots 0 and 1, V: slots 2 and 3
+        f32x4 s[4][2], next[4][2];
+        int now = entry(0);
+        copy(now, false, 0);
+        if (count > 1) copy(entry(1), false, 1);
+        copy(now, true, 2);
+        arrive();
+        scores(0, s);
+        for (int i = 0; i < count; ++i) {
+            if (i > 0) arrive();                       // K_{i+1} and V_i are there, and nobody reads K_i and V_{i-1} any more
+            else __syncthreads();
+            if (i + 2 < count) copy(entry(i + 2), false, i & 1);
+            if (i + 1 < count) copy(entry(i + 1), true, 2 + ((i + 1) & 1));
+            if constexpr (CAP) {                       // (before the mask: what is hidden is not -cap)
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+            }
+            if (now & 1 << 30) {
+                mask(now, s);
+                partly = true;
+            }
+            // a score far above the reference of its query: the reference moves up to the largest
+            float most[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                most[q] = s[0][q][0];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most[q] = fmaxf(most[q], s[kt][q][r]);
+                if constexpr (!CAP) most[q] *= scale;
+            }
+            if (__builtin_amdgcn_ballot_w64(most[0] > m[0] + 8.f || most[1] > m[1] + 8.f) != 0ull) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    float top = fmaxf(most[q], __shfl_xor(most[q], 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    top = fmaxf(top, m[q]);
+                    const float lower = __builtin_amdgcn_exp2f(m[q] - top);
+                    m[q] = top;
+                    sums[q] *= lower;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) acc[d][q] *= lower;
+                }
+            }
+            if (i + 1 < count) scores((i + 1) & 1, next);
+            bf16x8 w[2][2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = s[2 * half + e / 4][q][e % 4];
+                        w[half][q][e] = (__bf16)__builtin_amdgcn_exp2f(CAP ? x - m[q] : __builtin_fmaf(x, scale, -m[q]));
+                    }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[half][q], sums[q], 0, 0, 0);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    lds_char* v = (lds_char*)lds + (2 + (i & 1)) * L::BYTES + half * 32 * L::RB + vat[d];
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)v), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + 16 * L::RB));
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) acc[d][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[half][q], acc[d][q], 0, 0, 0);
+                }
+            }
+            if (i + 1 < count) {
+                now = entry(i + 1);
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) s[kt][q] = next[kt][q];
+            }
+        }
+        __syncthreads();                               // before the list and the slots serve the next tiles
+    }
+
+    // Results.  A weight of 0 times an infinity or NaN in a tile that not every query sees whole is NaN: such rows again, key by key.
+    unsigned again = 0;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int row = q0 + 16 * q + n;
+        const float inverse = 1.f / sums[q][0];
+        float all = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) all = __builtin_fmaf(acc[d][q][r], 0.f, all);
+        const unsigned long long bad = partly ? __builtin_amdgcn_ballot_w64(all != 0.f && row < length && doc[q] >= 0) : 0ull;
+        const unsigned rows = (unsigned)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu;
+        again |= rows << (16 * q);
+        if (row >= length || (rows >> n & 1) != 0) continue;
+        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * g;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            bf16x4v out;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out[r] = (__bf16)(doc[q] >= 0 ? acc[d][q][r] * inverse : 0.f);
+            *(bf16x4v*)(o + 32 * d) = out;
+        }
+    }
+    again = __builtin_amdgcn_readfirstlane(again);
+    while (again != 0) {
+        const int i = __builtin_ctz(again);
+        again &= again - 1;
+        row_by_keys<D>(p, b, h, q0 + i + (second ? p.n0 : 0), lane);
     }
 }
 
@@ -119,7 +464,7 @@ extern "C" {
 size_t rapid_attn_packed_workspace_bytes(int B, int H, int N, int D)
 {
     if (B <= 0 || H <= 0 || N <= 0 || N > (1 << 22) || (long long)B * H > 524287 || (D != 64 && D != 128)) return 0;
-    return 16;
+    return (size_t)B * ((N + TILE - 1) / TILE + 1) * sizeof(Known);       // (a tile more where there are two segments)
 }
 
 int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B, int H, int D, const int* document,
@@ -166,10 +511,17 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     p.cap = cap * LOG2E;
     p.scale = cap > 0.f ? 2.f * LOG2E * scale / cap : scale * LOG2E;
-    const long long groups = ((long long)B * H * N + 3) / 4;
-    const dim3 grid((unsigned)(groups < (1 << 20) ? groups : 1 << 20));
-    if (D == 64) hipLaunchKernelGGL(attn_packed_simple_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, p);
-    else hipLaunchKernelGGL(attn_packed_simple_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, p);
+    const int n1 = p.N - p.n0;
+    p.tiles0 = (p.n0 + TILE - 1) / TILE;
+    p.tiles = p.tiles0 + (n1 + TILE - 1) / TILE;
+    p.groups0 = (p.n0 + ROWS - 1) / ROWS;
+    p.groups1 = (n1 + ROWS - 1) / ROWS;
+    p.known = (Known*)workspace;
+    hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 3) / 4), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
+    const dim3 grid((unsigned)(B * H) * (unsigned)(p.groups0 + p.groups1));
+    auto kernel = D == 64 ? cap > 0.f ? attn_packed_kernel<64, true> : attn_packed_kernel<64, false>
+                          : cap > 0.f ? attn_packed_kernel<128, true> : attn_packed_kernel<128, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(WAVES * 64), 0, (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? RAPID_OK : RAPID_ERR_DEVICE;
 }
 
