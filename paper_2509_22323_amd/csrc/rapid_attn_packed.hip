@@ -4,6 +4,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "rapid_internal.h"
 #include "rapid_packed.h"
 
@@ -189,15 +191,22 @@ __device__ __forceinline__ void arrive()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// A tile that is visited: where it lies, and what else is asked of it.
+struct Visit {
+    unsigned low, high;                                // address of its keys: 48 bits; of `high` bit 31: not every query sees it whole; bit 30: second segment
+    int bytes;                                         // from its first to the end of its last row
+    int token;                                         // its first one in the joint sequence, and (rows - 1) << 24
+};
+
 template <int D, bool CAP>
 __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams p)
 {
     typedef Lds<D> L;
     constexpr int KS = D / 32, DT = D / 16;
-    constexpr int LIST = 1024;                         // tiles that are listed at a time
-    __shared__ __align__(1024) char lds[4 * L::BYTES];
-    __shared__ int list[LIST + 1];
-    __shared__ int found[WAVES + 1];
+    constexpr int LIST = 512;                          // tiles that are listed at a time
+    __shared__ __align__(1024) char lds[4 * L::BYTES + 4 * TILE * 4];
+    __shared__ __align__(16) Visit list[LIST];
+    __shared__ int found[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
 
     // which rows
@@ -237,7 +246,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
 
     // copies of a tile: this lane's rows and chunks
     const unsigned lds_at = (unsigned)(size_t)(lds_char*)lds;
-    const int crow = wave * L::COPIES * L::PER + lane / (64 / L::PER);
+    const unsigned crow = wave * L::COPIES * L::PER + lane / (64 / L::PER);
     unsigned ck[L::COPIES], cv[L::COPIES];
 #pragma unroll
     for (int j = 0; j < L::COPIES; ++j) {
@@ -245,20 +254,32 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
         ck[j] = 16u * (c ^ L::turn_k(row));
         cv[j] = 16u * (c ^ L::turn_v(row));
     }
-    auto copy = [&](int entry, bool is_v, int slot) {
-        const int tile = entry & 0x3fffffff;
-        const bool s = tile >= p.tiles0;
-        const Side& from = p.side[s];
-        const int row = (s ? tile - p.tiles0 : tile) * TILE, rows = min((s ? p.N - p.n0 : p.n0) - row, TILE);
-        const unsigned long long base = (unsigned long long)((is_v ? from.v : from.k) + b * from.in_sb + h * from.in_sh + (long long)row * from.in_sn);
-        const i32x4 buffer = {(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), (rows - 1) * from.in_sn + L::RB, 0x00020000};
-        const unsigned at = crow * from.in_sn;
+    const unsigned stride0 = p.side[0].in_sn, stride1 = p.side[1].in_sn;
+    const long long delta0 = p.side[0].v - p.side[0].k, delta1 = p.side[1].v - p.side[1].k;
+    const int* const documents = p.document + b * p.document_sb;
+    const int* const orders = p.order ? p.order + b * p.order_sb : nullptr;
+    auto copy = [&](const Visit& e, auto is_v, auto slot) {
+        constexpr bool V = is_v.value;
+        const bool s = (e.high >> 30 & 1) != 0;
+        const unsigned sn = s ? stride1 : stride0;
+        unsigned long long base = (unsigned long long)(e.high & 0xffffu) << 32 | e.low;
+        if constexpr (V) base += (unsigned long long)(s ? delta1 : delta0);
+        const i32x4 buffer = {(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), e.bytes, 0x00020000};
+        const unsigned at = __umul24(crow, sn);
 #pragma unroll
         for (int j = 0; j < L::COPIES; ++j) {
-            const unsigned off = at + (unsigned)(j * L::PER) * from.in_sn + (is_v ? cv[j] : ck[j]);
-            const unsigned dst = lds_at + slot * L::BYTES + (wave * L::COPIES + j) * 1024;
+            const unsigned off = at + (unsigned)(j * L::PER) * sn + (V ? cv[j] : ck[j]);
+            const unsigned dst = lds_at + slot.value * L::BYTES + (wave * L::COPIES + j) * 1024;
             if (j == 0) copy_1k<true>(buffer, off, dst);
             else copy_1k<false>(buffer, off, dst);
+        }
+        if constexpr (V) {                             // with the documents and orders of its tokens, 4 bytes a lane
+            if ((int)e.high < 0 && wave < 2 && (wave == 0 || orders)) {
+                const unsigned long long from = (unsigned long long)((wave == 0 ? documents : orders) + (e.token & 0xffffff));
+                const i32x4 words = {(int)(unsigned)from, (int)((unsigned)(from >> 32) & 0xffffu), 4 * ((e.token >> 24) + 1), 0x00020000};
+                const unsigned dst = lds_at + 4 * L::BYTES + (2 * (slot.value - 2) + wave) * 4 * TILE, off = 4u * lane;
+                asm volatile("s_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(words));
+            }
         }
     };
 
@@ -279,15 +300,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
 
     typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+    typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const float scale = p.scale, cap = p.cap;
 
-    auto scores = [&](int slot, f32x4 (&s)[4][2]) {
+    auto scores = [&](auto slot, f32x4 (&s)[4][2]) {
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const bf16x8 kf = *(lds_bf16x8*)((lds_char*)lds + slot * L::BYTES + kt * 16 * L::RB + kat[k]);
+                const bf16x8 kf = *(lds_bf16x8*)((lds_char*)lds + slot.value * L::BYTES + kt * 16 * L::RB + kat[k]);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const f32x4 none = {0.f, 0.f, 0.f, 0.f};
@@ -296,23 +319,101 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
             }
         }
     };
-    auto mask = [&](int entry, f32x4 (&s)[4][2]) {
-        const int tile = entry & 0x3fffffff;
-        const bool second = tile >= p.tiles0;
-        const int row = (second ? tile - p.tiles0 : tile) * TILE, rows = (second ? p.N - p.n0 : p.n0) - row;
-        const int* document = p.document + b * p.document_sb + (second ? p.n0 : 0) + row;
-        const int* order = p.order ? p.order + b * p.order_sb + (second ? p.n0 : 0) + row : nullptr;
+    auto mask = [&](const Visit& e, auto slot, f32x4 (&s)[4][2]) {
+        lds_char* const at = (lds_char*)lds + 4 * L::BYTES + 2 * slot.value * 4 * TILE + 16 * g;
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < 4; ++kt) {
+            const i32x4 d = *(lds_i32x4*)(at + 64 * kt);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int key = 16 * kt + 4 * g + r, at = min(key, rows - 1);
-                const int d = document[at], o = order ? order[at] : 0;
+            for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) s[kt][q][r] = key < rows && d == doc[q] && o <= turn[q] ? s[kt][q][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[kt][q][r] = d[r] == doc[q] ? s[kt][q][r] : -INFINITY;
+        }
+        if (orders) {
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                const i32x4 o = *(lds_i32x4*)(at + 4 * TILE + 64 * kt);
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[kt][q][r] = o[r] <= turn[q] ? s[kt][q][r] : -INFINITY;
             }
+        }
+        const int left = (e.token >> 24) + 1 - 4 * g;  // (rows that the tile does not have have come as zeros)
+        if ((e.token >> 24) != TILE - 1) {
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[kt][q][r] = 16 * kt + r < left ? s[kt][q][r] : -INFINITY;
+        }
     };
-    const float scale = p.scale, cap = p.cap;
+    // The weights of a tile whose scores are s, beside the scores of the next one, and what they add.
+    auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], bool another, auto turn_) {
+        constexpr int T = turn_.value;                 // K of this tile in slot T, V in slot 2 + T
+        if constexpr (CAP) {                           // (before the mask: what is hidden is not -cap)
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+        }
+        if ((int)e.high < 0) {
+            mask(e, turn_, s);
+            partly = true;
+        }
+        // a score far above the reference of its query: the reference moves up to the largest
+        float most[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            most[q] = s[0][q][0];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) most[q] = fmaxf(most[q], s[kt][q][r]);
+            if constexpr (!CAP) most[q] *= scale;
+        }
+        if (__builtin_amdgcn_ballot_w64(most[0] > m[0] + 8.f || most[1] > m[1] + 8.f) != 0ull) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float top = fmaxf(most[q], __shfl_xor(most[q], 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                top = fmaxf(top, m[q]);
+                const float lower = __builtin_amdgcn_exp2f(m[q] - top);
+                m[q] = top;
+                sums[q] *= lower;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[d][q] *= lower;
+            }
+        }
+        (void)another;                                 // (behind the last tile: scores of what is there, which nobody looks at)
+        scores(std::integral_constant<int, 1 - T>(), next);
+        bf16x8 w[2][2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = s[2 * half + i / 4][q][i % 4];
+                    w[half][q][i] = (__bf16)__builtin_amdgcn_exp2f(CAP ? v - m[q] : __builtin_fmaf(v, scale, -m[q]));
+                }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[half][q], sums[q], 0, 0, 0);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                lds_char* v = (lds_char*)lds + (2 + T) * L::BYTES + half * 32 * L::RB + vat[d];
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)v), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + 16 * L::RB));
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int q = 0; q < 2; ++q) acc[d][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[half][q], acc[d][q], 0, 0, 0);
+            }
+        }
+    };
 
     const int tiles = p.tiles;
     for (int from = 0; from < tiles; from += LIST) {
@@ -332,95 +433,63 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                 if (w < wave) before += found[w];
                 count += found[w];
             }
-            if (how != NONE) list[before + __popcll(some & ((1ull << lane) - 1ull))] = tile | (how == SOME ? 1 << 30 : 0);
+            if (how != NONE) {
+                const bool s = tile >= p.tiles0;
+                const Side& of = p.side[s];
+                const int row = (s ? tile - p.tiles0 : tile) * TILE, rows = min((s ? p.N - p.n0 : p.n0) - row, TILE);
+                const unsigned long long at = (unsigned long long)(of.k + b * of.in_sb + h * of.in_sh + (long long)row * of.in_sn);
+                list[before + __popcll(some & ((1ull << lane) - 1ull))] = Visit{
+                    (unsigned)at, (unsigned)(at >> 32 & 0xffffu) | (how == SOME ? 1u << 31 : 0u) | (s ? 1u << 30 : 0u),
+                    (rows - 1) * of.in_sn + L::RB, (s ? p.n0 : 0) + row | (rows - 1) << 24};
+            }
         }
         __syncthreads();
         count = __builtin_amdgcn_readfirstlane(count);
         if (count == 0) continue;
-        auto entry = [&](int i) { return __builtin_amdgcn_readfirstlane(list[i]); };
+        auto visit = [&](int i) {
+            const Visit e = list[i];
+            return Visit{(unsigned)__builtin_amdgcn_readfirstlane(e.low), (unsigned)__builtin_amdgcn_readfirstlane(e.high),
+                         __builtin_amdgcn_readfirstlane(e.bytes), __builtin_amdgcn_readfirstlane(e.token)};
+        };
+        constexpr std::integral_constant<int, 0> zero;
+        constexpr std::integral_constant<int, 1> one;
+        constexpr std::integral_constant<int, 2> two;
+        constexpr std::integral_constant<int, 3> three;
+        constexpr std::true_type values;
+        constexpr std::false_type keys;
 
         // K: slots 0 and 1, V: slots 2 and 3
-        f32x4 s[4][2], next[4][2];
-        int now = entry(0);
-        copy(now, false, 0);
-        if (count > 1) copy(entry(1), false, 1);
-        copy(now, true, 2);
+        f32x4 even[4][2], odd[4][2];
+        Visit now = visit(0), then = count > 1 ? visit(1) : now;
+        copy(now, keys, zero);
+        copy(now, values, two);
+        if (count > 1) copy(then, keys, one);
         arrive();
-        scores(0, s);
-        for (int i = 0; i < count; ++i) {
-            if (i > 0) arrive();                       // K_{i+1} and V_i are there, and nobody reads K_i and V_{i-1} any more
-            else __syncthreads();
-            if (i + 2 < count) copy(entry(i + 2), false, i & 1);
-            if (i + 1 < count) copy(entry(i + 1), true, 2 + ((i + 1) & 1));
-            if constexpr (CAP) {                       // (before the mask: what is hidden is not -cap)
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+        scores(zero, even);
+        __syncthreads();
+        for (int i = 0;; i += 2) {
+            // K_{i+1} and V_i are there, and nobody reads K_i and V_{i-1} any more
+            Visit later = then;
+            if (i + 2 < count) {
+                later = visit(i + 2);
+                copy(later, keys, zero);
             }
-            if (now & 1 << 30) {
-                mask(now, s);
-                partly = true;
+            if (i + 1 < count) copy(then, values, three);
+            step(now, even, odd, i + 1 < count, zero);
+            if (i + 1 >= count) break;
+            arrive();
+            now = later;
+            if (i + 3 < count) {
+                later = visit(i + 3);
+                copy(later, keys, one);
             }
-            // a score far above the reference of its query: the reference moves up to the largest
-            float most[2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                most[q] = s[0][q][0];
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) most[q] = fmaxf(most[q], s[kt][q][r]);
-                if constexpr (!CAP) most[q] *= scale;
-            }
-            if (__builtin_amdgcn_ballot_w64(most[0] > m[0] + 8.f || most[1] > m[1] + 8.f) != 0ull) {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float top = fmaxf(most[q], __shfl_xor(most[q], 16, 64));
-                    top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    top = fmaxf(top, m[q]);
-                    const float lower = __builtin_amdgcn_exp2f(m[q] - top);
-                    m[q] = top;
-                    sums[q] *= lower;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) acc[d][q] *= lower;
-                }
-            }
-            if (i + 1 < count) scores((i + 1) & 1, next);
-            bf16x8 w[2][2];
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = s[2 * half + e / 4][q][e % 4];
-                        w[half][q][e] = (__bf16)__builtin_amdgcn_exp2f(CAP ? x - m[q] : __builtin_fmaf(x, scale, -m[q]));
-                    }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[half][q], sums[q], 0, 0, 0);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    lds_char* v = (lds_char*)lds + (2 + (i & 1)) * L::BYTES + half * 32 * L::RB + vat[d];
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)v), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + 16 * L::RB));
-                    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) acc[d][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[half][q], acc[d][q], 0, 0, 0);
-                }
-            }
-            if (i + 1 < count) {
-                now = entry(i + 1);
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) s[kt][q] = next[kt][q];
-            }
+            if (i + 2 < count) copy(now, values, two);
+            step(then, odd, even, i + 2 < count, one);
+            if (i + 2 >= count) break;
+            arrive();
+            then = later;
         }
-        __syncthreads();                               // before the list and the slots serve the next tiles
+        arrive();                                      // before the list and the slots serve the next tiles
     }
 
     // Results.  A weight of 0 times an infinity or NaN in a tile that not every query sees whole is NaN: such rows again, key by key.
