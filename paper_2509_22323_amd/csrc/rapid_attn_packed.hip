@@ -33,6 +33,7 @@ struct PackedParams {
     int n0, N, B, H;                                   // tokens of the first segment, of both
     int tiles0, tiles, groups0, groups1;               // tiles of the first segment, of both; groups of 128 queries of each
     Known* known;                                      // [B, tiles]
+    int* sorted;                                       // [B, groups], most work first, or null
     float scale;                                       // of a score: capped / log2(e), else as exponent of 2
     float cap;                                         // as exponent of 2; 0: none
 };
@@ -121,6 +122,25 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int smallest(const Known& k) { return k.first < 0 ? ~k.first : k.first; }
 
+template <int CTRL>
+__device__ __forceinline__ int moved(int v)
+{
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+}
+// f over the values of the wavefront, in every lane
+template <class F>
+__device__ __forceinline__ int over_lanes(int v, F f)
+{
+    v = f(v, moved<0xB1>(v));                          // lane ^ 1
+    v = f(v, moved<0x4E>(v));                          // lane ^ 2
+    v = f(v, moved<0x141>(v));                         // 7 - lane of every 8
+    v = f(v, moved<0x140>(v));                         // 15 - lane of every 16
+    auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f((int)a[0], (int)a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return f((int)b[0], (int)b[1]);
+}
+
 // Of tile `tile` of a sample, by a wavefront.
 __device__ __forceinline__ Known known_of(const PackedParams& p, int b, int tile, int lane)
 {
@@ -129,13 +149,12 @@ __device__ __forceinline__ Known known_of(const PackedParams& p, int b, int tile
     const int t = min(row, n - 1) + (second ? p.n0 : 0);
     const int d = p.document[b * p.document_sb + t], o = p.order ? p.order[b * p.order_sb + t] : 0;
     const bool there = row < n && d >= 0;
-    Known k = {there ? d : INT_MAX, there ? d : -1, there ? o : INT_MAX, there ? o : INT_MIN};
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-        k.first = min(k.first, __shfl_xor(k.first, x, 64));
-        k.last = max(k.last, __shfl_xor(k.last, x, 64));
-        k.early = min(k.early, __shfl_xor(k.early, x, 64));
-        k.late = max(k.late, __shfl_xor(k.late, x, 64));
+    auto least = [](int a, int b) { return min(a, b); };
+    auto most = [](int a, int b) { return max(a, b); };
+    Known k = {over_lanes(there ? d : INT_MAX, least), over_lanes(there ? d : -1, most), 0, 0};
+    if (p.order) {
+        k.early = over_lanes(there ? o : INT_MAX, least);
+        k.late = over_lanes(there ? o : INT_MIN, most);
     }
     if (__builtin_amdgcn_ballot_w64(!there) != 0ull) k.first = ~k.first;
     return k;
@@ -148,6 +167,54 @@ __device__ __forceinline__ int sees(const Known& q, const Known& k)
     const int qf = smallest(q), kf = smallest(k);
     if (q.last < 0 || k.last < 0 || kf > q.last || k.last < qf || k.early > q.late) return NONE;
     return k.first == k.last && qf == q.last && k.first == qf && k.late <= q.early ? ALL : SOME;
+}
+
+// What is known of the queries of group `group` (of the tiles in `known`).
+__device__ __forceinline__ Known known_of_group(const PackedParams& p, const Known* known, int group)
+{
+    const bool second = group >= p.groups0;
+    const int tile = second ? p.tiles0 + 2 * (group - p.groups0) : 2 * group;
+    Known mine = known[tile];
+    if (tile + 1 < (second ? p.tiles : p.tiles0)) {
+        const Known k = known[tile + 1];
+        mine.first = min(smallest(mine), smallest(k));
+        mine.last = max(mine.last, k.last);
+        mine.early = min(mine.early, k.early);
+        mine.late = max(mine.late, k.late);
+    }
+    return mine;
+}
+
+// What is known of all tiles, and the groups of a sample in the order of what they have to do, most first: workgroups go to the CUs in
+// turn as these get free, so that what is left for last is short.  A workgroup a sample, of PLANNED tiles at most.
+constexpr int PLANNED = 1026;
+__global__ __launch_bounds__(1024) void packed_plan_kernel(PackedParams p)
+{
+    __shared__ __align__(16) Known known[PLANNED];
+    __shared__ int visits[PLANNED / 2 + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = p.groups0 + p.groups1, b = blockIdx.x;
+    for (int tile = wave; tile < p.tiles; tile += 16) {
+        const Known k = known_of(p, b, tile, lane);
+        if (lane == 0) {
+            known[tile] = k;
+            p.known[(long long)b * p.tiles + tile] = k;
+        }
+    }
+    __syncthreads();
+    for (int group = wave; group < per; group += 16) {
+        const Known mine = known_of_group(p, known, group);
+        int count = 0;
+        for (int t = 0; t < p.tiles; t += 64)
+            count += __popcll(__builtin_amdgcn_ballot_w64(t + lane < p.tiles && sees(mine, known[min(t + lane, p.tiles - 1)]) != NONE));
+        if (lane == 0) visits[group] = count;
+    }
+    __syncthreads();
+    for (int group = tid; group < per; group += 1024) {
+        int before = 0;
+        const int own = visits[group];
+        for (int i = 0; i < per; ++i) before += visits[i] > own || (visits[i] == own && i < group);
+        p.sorted[(long long)b * per + before] = group;
+    }
 }
 
 // What is known of all tiles, a wavefront each.
@@ -209,25 +276,29 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
     __shared__ int found[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
 
-    // which rows
-    const int per = p.groups0 + p.groups1;
-    const unsigned items = (unsigned)(p.B * p.H) * per, each = items / 8, more = items % 8, x = blockIdx.x % 8;
-    const unsigned item = x * each + min(x, more) + blockIdx.x / 8;
-    const int head = __builtin_amdgcn_readfirstlane(item / per), b = __builtin_amdgcn_readfirstlane(head / p.H), h = head - b * p.H;
-    const int group = per - 1 - (int)(item - (unsigned)head * per);
+    // Which rows: 8 heads at a time, an XCD each, so that an L2 holds the keys and values of few of them; of these the groups with most to
+    // do first; the heads that are left over are dealt out to all XCDs.
+    const int per = p.groups0 + p.groups1, pairs = p.B * p.H, whole = pairs / 8, rest = pairs % 8;
+    const int xcd = blockIdx.x % 8, turn_in = blockIdx.x / 8;
+    int head, rank;
+    if (turn_in < whole * per) {
+        rank = turn_in / whole;
+        head = xcd + 8 * (turn_in - rank * whole);
+    } else {
+        const int i = (turn_in - whole * per) * 8 + xcd;
+        if (i >= rest * per) return;
+        rank = i / rest;
+        head = 8 * whole + i - rank * rest;
+    }
+    head = __builtin_amdgcn_readfirstlane(head);
+    rank = __builtin_amdgcn_readfirstlane(rank);
+    const int b = __builtin_amdgcn_readfirstlane(head / p.H), h = head - b * p.H;
+    const int group = p.sorted ? p.sorted[(long long)b * per + rank] : per - 1 - rank;
     const bool second = group >= p.groups0;
     const Side& own = p.side[second];
     const int length = second ? p.N - p.n0 : p.n0, row0 = (second ? group - p.groups0 : group) * ROWS;
     const Known* known = p.known + (long long)b * p.tiles;
-    const int tile0 = (second ? p.tiles0 : 0) + row0 / TILE;
-    Known mine = known[tile0];
-    if (row0 + TILE < length) {
-        const Known k = known[tile0 + 1];
-        mine.first = min(smallest(mine), smallest(k));
-        mine.last = max(mine.last, k.last);
-        mine.early = min(mine.early, k.early);
-        mine.late = max(mine.late, k.late);
-    }
+    const Known mine = known_of_group(p, known, group);
 
     // queries: lane (n, g) holds elements 32 t + 8 g .. + 7 of query 16 q + n
     const int q0 = row0 + 32 * wave;
@@ -533,7 +604,8 @@ extern "C" {
 size_t rapid_attn_packed_workspace_bytes(int B, int H, int N, int D)
 {
     if (B <= 0 || H <= 0 || N <= 0 || N > (1 << 22) || (long long)B * H > 524287 || (D != 64 && D != 128)) return 0;
-    return (size_t)B * ((N + TILE - 1) / TILE + 1) * sizeof(Known);       // (a tile more where there are two segments)
+    const size_t tiles = (N + TILE - 1) / TILE + 1, groups = (N + ROWS - 1) / ROWS + 1;        // (one more where there are two segments)
+    return (size_t)B * (tiles * sizeof(Known) + (tiles <= PLANNED ? (groups + 3) / 4 * 16 : 0));
 }
 
 int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B, int H, int D, const int* document,
@@ -586,8 +658,14 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     p.groups0 = (p.n0 + ROWS - 1) / ROWS;
     p.groups1 = (n1 + ROWS - 1) / ROWS;
     p.known = (Known*)workspace;
-    hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 3) / 4), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
-    const dim3 grid((unsigned)(B * H) * (unsigned)(p.groups0 + p.groups1));
+    const int per = p.groups0 + p.groups1, pairs = B * H;
+    if (p.tiles <= PLANNED) {
+        p.sorted = (int*)(p.known + (size_t)B * p.tiles);
+        hipLaunchKernelGGL(packed_plan_kernel, dim3((unsigned)B), dim3(1024), 0, (hipStream_t)stream, p);
+    } else {
+        hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 3) / 4), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
+    }
+    const dim3 grid(8u * (unsigned)(pairs / 8 * per + (pairs % 8 * per + 7) / 8));
     auto kernel = D == 64 ? cap > 0.f ? attn_packed_kernel<64, true> : attn_packed_kernel<64, false>
                           : cap > 0.f ? attn_packed_kernel<128, true> : attn_packed_kernel<128, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(WAVES * 64), 0, (hipStream_t)stream, p);
