@@ -36,6 +36,7 @@ struct PackedParams {
     int* sorted;                                       // [B, groups], most work first, or null
     float scale;                                       // of a score: capped / log2(e), else as exponent of 2
     float cap;                                         // as exponent of 2; 0: none
+    float small, series[5];                            // of a capped score: see series()
 };
 
 __device__ __forceinline__ float most_of_lanes(float v)
@@ -57,6 +58,13 @@ __device__ __forceinline__ float exponent(float s, float scale, float cap)
     if (cap == 0.f) return s * scale;
     // cap tanh(u) = cap - 2 cap / (1 + exp(2 u)), scale = 2 log2(e) scale' / cap'
     return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * scale)), cap);
+}
+
+// The same over s, where |s| <= p.small: tanh(u) / u as a polynomial in u^2, fitted to 1.0e-6 of it up to u = 0.8.
+__device__ __forceinline__ float series(const PackedParams& p, float s)
+{
+    const float t = s * s;
+    return __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(p.series[4], t, p.series[3]), t, p.series[2]), t, p.series[1]), t, p.series[0]);
 }
 
 // One row of the output by one wavefront, key by key: a lane a key for the scores, D / 64 elements of the output a lane.
@@ -424,12 +432,29 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
     auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], bool another, auto turn_) {
         constexpr int T = turn_.value;                 // K of this tile in slot T, V in slot 2 + T
         if constexpr (CAP) {                           // (before the mask: what is hidden is not -cap)
+            float size = 0.f;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+                    for (int r = 0; r < 4; ++r) size = fmaxf(size, fabsf(s[kt][q][r]));
+            const bool small = __builtin_amdgcn_ballot_w64(size > p.small) == 0ull;
+            if (__builtin_expect(small, 1)) {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[kt][q][r] *= series(p, s[kt][q][r]);
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+            }
         }
         if ((int)e.high < 0) {
             mask(e, turn_, s);
@@ -460,8 +485,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
             }
         }
         (void)another;                                 // (behind the last tile: scores of what is there, which nobody looks at)
-        scores(std::integral_constant<int, 1 - T>(), next);
         bf16x8 w[2][2];
+        scores(std::integral_constant<int, 1 - T>(), next);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -652,6 +677,13 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
     p.cap = cap * LOG2E;
     p.scale = cap > 0.f ? 2.f * LOG2E * scale / cap : scale * LOG2E;
+    // (the polynomial's factors are numbers of fp32 for all but caps that are out of proportion to the scale)
+    const double u = cap > 0.f ? (double)scale / cap : 0.0;
+    if (u > 0x1p-12 && u < 0x1p12) {
+        constexpr double TANH[5] = {0.999998994, -0.33325372, 0.132305656, -0.0491801422, 0.0121001386};
+        p.small = (float)(0.8 / u);
+        for (int i = 0; i < 5; ++i) p.series[i] = (float)(TANH[i] * p.cap * pow(u, 2 * i + 1));
+    }
     const int n1 = p.N - p.n0;
     p.tiles0 = (p.n0 + TILE - 1) / TILE;
     p.tiles = p.tiles0 + (n1 + TILE - 1) / TILE;
