@@ -428,8 +428,27 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                     for (int r = 0; r < 4; ++r) s[kt][q][r] = 16 * kt + r < left ? s[kt][q][r] : -INFINITY;
         }
     };
-    // The weights of a tile whose scores are s, beside the scores of the next one, and what they add.
-    auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], bool another, auto turn_) {
+    auto each = [](auto a, auto b, auto&& f) {         // f with the numbers a .. b - 1 as constants
+        auto go = [&](auto self, auto i) {
+            if constexpr (i.value < b.value) {
+                f(i);
+                self(self, std::integral_constant<int, i.value + 1>());
+            }
+        };
+        go(go, a);
+    };
+    auto largest = [&](const f32x4 (&s)[4][2], int q) {
+        float v = s[0][q][0];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v = fmaxf(v, s[kt][q][r]);
+        return v;
+    };
+    float most[2];                                     // of this lane's scores of a tile
+    // The weights of a tile whose scores are s, and what they add, beside the scores of the next one.  Items: one operand from LDS, requested
+    // AHEAD items before, and the matrix instructions of both groups of queries; behind each a quarter or two of the work on a pair of weights.
+    auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], auto turn_) {
         constexpr int T = turn_.value;                 // K of this tile in slot T, V in slot 2 + T
         if constexpr (CAP) {                           // (before the mask: what is hidden is not -cap)
             float size = 0.f;
@@ -447,6 +466,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[kt][q][r] *= series(p, s[kt][q][r]);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) most[q] *= series(p, most[q]);
             } else {
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
@@ -454,23 +475,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) most[q] = exponent(most[q], scale, cap);
             }
         }
         if ((int)e.high < 0) {
             mask(e, turn_, s);
             partly = true;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) most[q] = largest(s, q);
         }
         // a score far above the reference of its query: the reference moves up to the largest
-        float most[2];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            most[q] = s[0][q][0];
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most[q] = fmaxf(most[q], s[kt][q][r]);
+        for (int q = 0; q < 2; ++q)
             if constexpr (!CAP) most[q] *= scale;
-        }
         if (__builtin_amdgcn_ballot_w64(most[0] > m[0] + 8.f || most[1] > m[1] + 8.f) != 0ull) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
@@ -484,31 +502,64 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                 for (int d = 0; d < DT; ++d) acc[d][q] *= lower;
             }
         }
-        (void)another;                                 // (behind the last tile: scores of what is there, which nobody looks at)
-        bf16x8 w[2][2];
-        scores(std::integral_constant<int, 1 - T>(), next);
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float v = s[2 * half + i / 4][q][i % 4];
-                    w[half][q][i] = (__bf16)__builtin_amdgcn_exp2f(CAP ? v - m[q] : __builtin_fmaf(v, scale, -m[q]));
-                }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int q = 0; q < 2; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[half][q], sums[q], 0, 0, 0);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                lds_char* v = (lds_char*)lds + (2 + T) * L::BYTES + half * 32 * L::RB + vat[d];
+        // Items 0 .. QK - 1: scores of the next tile (behind the last one: of what is there, which nobody looks at); QK .. : of 32 keys each,
+        // what the weights add.  Pairs of weights 0 .. 7 of the first 32 keys, 8 .. 15 of the others, each before the items that take them.
+        constexpr int QK = 4 * KS, PV = DT, ALL = QK + 2 * PV, AHEAD = 3, EARLY = 40;
+        bf16x8 f[AHEAD + 1];
+        unsigned w[2][2][4];
+        float x0, x1, e0, e1;
+        auto request = [&](auto item) {
+            constexpr int I = item.value;
+            if constexpr (I < QK) {
+                f[I % (AHEAD + 1)] = *(lds_bf16x8*)((lds_char*)lds + (1 - T) * L::BYTES + (I % 4) * 16 * L::RB + kat[I / 4]);
+            } else {
+                lds_char* v = (lds_char*)lds + (2 + T) * L::BYTES + ((I - QK) / PV) * 32 * L::RB + vat[(I - QK) % PV];
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)v), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + 16 * L::RB));
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int q = 0; q < 2; ++q) acc[d][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[half][q], acc[d][q], 0, 0, 0);
+                f[I % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
-        }
+        };
+        // a quarter of the work on a pair: exponents, first and second weight, both as bf16
+        auto quarter = [&](auto unit) {
+            constexpr int P = unit.value / 4, part = unit.value % 4, half = P / 8, q = P % 8 / 4, i = P % 4;
+            if constexpr (part == 0) {
+                const float a = s[2 * half + i / 2][q][2 * (i % 2)], b = s[2 * half + i / 2][q][2 * (i % 2) + 1];
+                x0 = CAP ? a - m[q] : __builtin_fmaf(a, scale, -m[q]);
+                x1 = CAP ? b - m[q] : __builtin_fmaf(b, scale, -m[q]);
+            } else if constexpr (part == 1) {
+                e0 = __builtin_amdgcn_exp2f(x0);
+            } else if constexpr (part == 2) {
+                e1 = __builtin_amdgcn_exp2f(x1);
+            } else {
+                const bf16x2 both = {(__bf16)e0, (__bf16)e1};
+                w[half][q][i] = __builtin_bit_cast(unsigned, both);
+            }
+        };
+        constexpr std::integral_constant<int, 0> begin;
+        each(begin, std::integral_constant<int, AHEAD>(), request);
+        each(begin, std::integral_constant<int, ALL>(), [&](auto item) {
+            constexpr int I = item.value, half = I < QK + PV ? 0 : 1;
+            if constexpr (I + AHEAD < ALL) request(std::integral_constant<int, I + AHEAD>());
+            each(begin, std::integral_constant<int, 2>(), [&](auto query) {
+                constexpr int q = query.value, at = 2 * I + q;     // 2 I + q: matrix instructions before this one
+                if constexpr (I < QK) {
+                    constexpr int kt = I % 4, k = I / 4;
+                    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+                    next[kt][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[I % (AHEAD + 1)], qf[q][k], k == 0 ? none : next[kt][q], 0, 0, 0);
+                } else {
+                    constexpr int d = (I - QK) % PV;
+                    const bf16x8 by = __builtin_bit_cast(bf16x8, w[half][q]);
+                    acc[d][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[I % (AHEAD + 1)], by, acc[d][q], 0, 0, 0);
+                    if constexpr (d == PV - 1) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, by, sums[q], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int M = 2 * QK, H = 2 * PV;
+                constexpr int from = at < M ? at * EARLY / M : at < M + H ? EARLY + (at - M) * (64 - EARLY) / H : 64;
+                constexpr int upto = at < M ? (at + 1) * EARLY / M : at < M + H ? EARLY + (at + 1 - M) * (64 - EARLY) / H : 64;
+                each(std::integral_constant<int, from>(), std::integral_constant<int, upto>(), quarter);
+                if constexpr (I == ALL - 2) most[q] = largest(next, q);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
     };
 
     const int tiles = p.tiles;
@@ -562,6 +613,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
         if (count > 1) copy(then, keys, one);
         arrive();
         scores(zero, even);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) most[q] = largest(even, q);
         __syncthreads();
         for (int i = 0;; i += 2) {
             // K_{i+1} and V_i are there, and nobody reads K_i and V_{i-1} any more
@@ -571,7 +624,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                 copy(later, keys, zero);
             }
             if (i + 1 < count) copy(then, values, three);
-            step(now, even, odd, i + 1 < count, zero);
+            step(now, even, odd, zero);
             if (i + 1 >= count) break;
             arrive();
             now = later;
@@ -580,7 +633,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams
                 copy(later, keys, one);
             }
             if (i + 2 < count) copy(now, values, two);
-            step(then, odd, even, i + 2 < count, one);
+            step(then, odd, even, one);
             if (i + 2 >= count) break;
             arrive();
             then = later;
