@@ -183,6 +183,7 @@ class _NoNative:
         return None
     dense = block_sparse = joint = joint_select = select = store = reuse = _takes_nothing
     linear = modulate = table = qk_norm_rope = rope = _takes_nothing
+    quantize = modulate8 = linear8 = packed_attention = _takes_nothing
 
 
 def _load_native():
@@ -210,7 +211,8 @@ def _load_native():
     module.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "rapid_attn_dense", "rapid_attn_block_sparse", "rapid_attn_joint", "rapid_attn_joint_select", "rapid_mask_select",
         "rapid_cache_store", "rapid_cache_reuse", "rapid_linear", "rapid_linear_workspace_bytes", "rapid_norm_modulate",
-        "rapid_rope_table", "rapid_qk_norm_rope", "rapid_rope")), RopeAxis)
+        "rapid_rope_table", "rapid_qk_norm_rope", "rapid_rope", "rapid_quantize_rows", "rapid_norm_modulate_int8", "rapid_linear_int8",
+        "rapid_linear_int8_workspace_bytes", "rapid_attn_packed")), RopeAxis)
     _native = module
     return module
 
@@ -878,6 +880,10 @@ def rapid_quantize_rows(x, q, scale):
     """q, scale <- the rows of x as 8-bit integers: q = round(127 x / m), ties to even, scale = m / 127, m the row's largest magnitude.
     x: CUDA bf16 [B,n,K] (or [n,K]), q: int8 of its shape, last dimensions contiguous; scale: float32 [B,n] (or [n]) contiguous.
     Weights are quantised by the same call.  Inference only: not recorded by autograd, no gradients.  Returns (q, scale)."""
+    status = (_native or _load_native()).quantize(x, q, scale)
+    if status is not None:
+        _check_packed(status)
+        return q, scale
     xr, B, n, K = _rows("x", x)
     device = x.get_device()
     qr, *shape = _rows("q", q, device, "int8")
@@ -895,6 +901,10 @@ def rapid_norm_modulate_int8(x, q, q_scale, scale=None, shift=None, eps=1e-6, do
     x, q, q_scale as there; scale, shift: CUDA bf16 [B,C] or [C], both or neither; with document (int32 [B,n], or [n], contiguous)
     they are [documents,C], numbered by it, and rows of no document (-1) are left as they were.
     Inference only: not recorded by autograd, no gradients.  Returns (q, q_scale)."""
+    status = (_native or _load_native()).modulate8(x, q, q_scale, scale, shift, eps, document)
+    if status is not None:
+        _check_packed(status)
+        return q, q_scale
     xr, B, n, C = _rows("x", x)
     device = x.get_device()
     qr, *shape = _rows("q", q, device, "int8")
@@ -927,6 +937,10 @@ def rapid_linear_int8(x, x_scale, weight, w_scale, out, bias=None, activation="n
     of no document (-1) are left as they were.  `workspace`: CUDA uint8 tensor of at least rapid_linear_int8_workspace_bytes(B*n, N, K)
     bytes; allocated with torch if None.  The same row of x gives the same bits in whatever call.
     Inference only: not recorded by autograd, no gradients.  Returns out."""
+    status = (_native or _load_native()).linear8(x, x_scale, weight, w_scale, out, bias, activation, gate, residual, document, workspace)
+    if status is not None:
+        _check_packed(status)
+        return out
     import torch
     xr, B, n, K = _rows("x", x, None, "int8")
     device = x.get_device()
@@ -990,6 +1004,11 @@ def rapid_attn_packed(segments, document, order=None, cap=0.0, scale=0.0, worksp
     tokens; cap > 0: scores s become cap * tanh(s / cap).  `workspace`: CUDA uint8 tensor of at least
     rapid_attn_packed_workspace_bytes(B, H, N, D) bytes; allocated with torch if None.
     Inference only: not recorded by autograd, no gradients.  Returns the o tensors."""
+    if workspace is not None:                     # (the native form allocates nothing)
+        status = (_native or _load_native()).packed_attention(segments, document, order, cap, scale, workspace)
+        if status is not None:
+            _check_packed(status)
+            return [seg[3] for seg in segments]
     import torch
     descr, B, H, N, D = _segments(segments)
     q0 = segments[0][0]

@@ -17,6 +17,7 @@
 #include "rapid_cache.h"
 #include "rapid_layer.h"
 #include "rapid_mask.h"
+#include "rapid_packed.h"
 
 namespace {
 
@@ -36,6 +37,11 @@ decltype(&rapid_norm_modulate) layer_modulate;
 decltype(&rapid_rope_table) layer_table;
 decltype(&rapid_qk_norm_rope) layer_qk;
 decltype(&rapid_rope) layer_rope;
+decltype(&rapid_quantize_rows) rows_quantize;
+decltype(&rapid_norm_modulate_int8) rows_modulate;
+decltype(&rapid_linear_int8) int8_linear;
+decltype(&rapid_linear_int8_workspace_bytes) int8_linear_bytes;
+decltype(&rapid_attn_packed) attn_packed;
 
 // A tensor of exactly that class with memory of its own on a GPU; else null.
 const at::Tensor* plain(PyObject* o)
@@ -318,9 +324,9 @@ struct Rows3 {
     rapid_rows rows;
     int B, n, width, device;
 };
-bool rows3(PyObject* o, Rows3& x)
+bool rows3(PyObject* o, Rows3& x, at::ScalarType type = at::kBFloat16)
 {
-    const at::Tensor* t = of(o, at::kBFloat16);
+    const at::Tensor* t = of(o, type);
     if (!t || (t->dim() != 2 && t->dim() != 3)) return false;
     const int d = (int)t->dim();
     x.B = 1;
@@ -508,12 +514,135 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n)
     return launch(x.device, [&](void* s) { return layer_rope(x.seg, x.n, x.B, x.H, x.D, x.table, x.table_stride, x.rot, x.layout, s); });
 }
 
+// ---- layers in 8 bits over packed sequences
+// None, or a contiguous tensor [B, n], or [n] where B is 1
+bool per_row(PyObject* o, at::ScalarType type, const Rows3& like, const void*& p)
+{
+    p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = packed(o, type, like.device);
+    if (!t) return false;
+    if (t->dim() == 2 ? t->size(0) != like.B || t->size(1) != like.n : t->dim() != 1 || like.B != 1 || t->size(0) != like.n) return false;
+    p = t->data_ptr();
+    return true;
+}
+// Rows of the conditioning's vectors: the samples, or the documents that vectors of two dimensions have (they have to agree), or any number.
+bool vector_rows(PyObject* const* a, int n, bool documents, const Rows3& like, Rows3& rows)
+{
+    rows = like;
+    if (!documents) return true;
+    rows.B = INT_MAX;
+    for (int i = 0; i < n; ++i) {
+        if (a[i] == Py_None) continue;
+        const at::Tensor* t = plain(a[i]);
+        int count;
+        if (!t) return false;
+        if (t->dim() != 2) continue;
+        if (!size(t->size(0), count) || (rows.B != INT_MAX && rows.B != count)) return false;
+        rows.B = count;
+    }
+    return true;
+}
+
+// (x, q, scale)
+PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows3 x, q;
+    const void* scale;
+    if (n != 3 || !rows3(a[0], x) || !rows3(a[1], q, at::kChar) || q.B != x.B || q.n != x.n || q.width != x.width || q.device != x.device) Py_RETURN_NONE;
+    if (!current(x.device) || a[2] == Py_None || !per_row(a[2], at::kFloat, x, scale)) Py_RETURN_NONE;
+    return launch(x.device, [&](void* s) { return rows_quantize(&x.rows, &q.rows, (float*)scale, x.B, x.n, x.width, s); });
+}
+
+// (x, q, q_scale, scale, shift, eps, document)
+PyObject* modulate8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows3 x, q, rows;
+    const void *q_scale, *scale, *shift, *document;
+    long long scale_stride, shift_stride;
+    float eps;
+    if (n != 7 || !rows3(a[0], x) || !rows3(a[1], q, at::kChar) || q.B != x.B || q.n != x.n || q.width != x.width || q.device != x.device) Py_RETURN_NONE;
+    if (!current(x.device) || a[2] == Py_None || !per_row(a[2], at::kFloat, x, q_scale) || !per_row(a[6], at::kInt, x, document)) Py_RETURN_NONE;
+    if (!vector_rows(a + 3, 2, document != nullptr, x, rows) || !vectors(a[3], rows, scale, scale_stride) || !vectors(a[4], rows, shift, shift_stride)) Py_RETURN_NONE;
+    if (!scale != !shift || !number(a[5], eps)) Py_RETURN_NONE;
+    return launch(x.device, [&](void* s) {
+        return rows_modulate(&x.rows, &q.rows, (float*)q_scale, scale, scale_stride, shift, shift_stride, (const int*)document, document ? rows.B : 0,
+                             x.B, x.n, x.width, eps, s);
+    });
+}
+
+// (x, x_scale, weight, w_scale, out, bias, activation, gate, residual, document, workspace or None where none is made use of)
+PyObject* linear8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows3 x, out, res, rows;
+    if (n != 11 || !rows3(a[0], x, at::kChar) || !rows3(a[4], out) || out.B != x.B || out.n != x.n || out.device != x.device || !current(x.device)) Py_RETURN_NONE;
+    const at::Tensor *w = of(a[2], at::kChar), *ws_scale = packed(a[3], at::kFloat, x.device);
+    if (!w || w->dim() != 2 || w->size(0) != out.width || w->size(1) != x.width || w->get_device() != x.device) Py_RETURN_NONE;
+    if ((w->stride(1) != 1 && x.width != 1) || !ws_scale || ws_scale->dim() != 1 || ws_scale->size(0) != out.width) Py_RETURN_NONE;
+    const void *x_scale, *document, *bias, *gate;
+    long long unused, gate_stride;
+    if (a[1] == Py_None || !per_row(a[1], at::kFloat, x, x_scale) || !per_row(a[9], at::kInt, x, document)) Py_RETURN_NONE;
+    if (!vectors(a[5], out, bias, unused) || (bias && THPVariable_Unpack(a[5]).dim() != 1)) Py_RETURN_NONE;
+    if (!vector_rows(a + 7, 1, document != nullptr, out, rows) || !vectors(a[7], rows, gate, gate_stride)) Py_RETURN_NONE;
+    const int activation = is(a[6], "none") ? RAPID_ACT_NONE : is(a[6], "silu") ? RAPID_ACT_SILU : is(a[6], "gelu_tanh") ? RAPID_ACT_GELU_TANH : -1;
+    if (activation < 0) Py_RETURN_NONE;
+    if (a[8] != Py_None && (!rows3(a[8], res) || res.B != out.B || res.n != out.n || res.width != out.width || res.device != x.device)) Py_RETURN_NONE;
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (a[10] != Py_None) {
+        const at::Tensor* t = plain(a[10]);
+        if (!t || !t->is_contiguous() || t->get_device() != x.device) Py_RETURN_NONE;
+        ws = t->data_ptr();
+        bytes = t->nbytes();
+    } else if (int8_linear_bytes((long long)x.B * x.n, out.width, x.width) != 0) Py_RETURN_NONE;
+    const void *weight = w->data_ptr(), *w_scale = ws_scale->data_ptr();
+    const long long w_stride = out.width > 1 ? w->stride(0) : x.width;
+    const rapid_rows* residual = a[8] != Py_None ? &res.rows : nullptr;
+    return launch(x.device, [&](void* s) {
+        return int8_linear(&x.rows, (const float*)x_scale, weight, w_stride, (const float*)w_scale, bias, &out.rows, activation, gate, gate_stride,
+                           residual, (const int*)document, document ? rows.B : 0, x.B, x.n, out.width, x.width, ws, bytes, s);
+    });
+}
+
+// int32 [B, N], or [N] (one for all samples), with a contiguous last dimension
+bool per_token(PyObject* o, const Joint& x, const int*& p, long long& stride)
+{
+    const at::Tensor* t = of(o, at::kInt);
+    if (!t || (t->dim() != 1 && t->dim() != 2) || t->get_device() != x.device) return false;
+    const int d = (int)t->dim();
+    if (t->size(d - 1) != x.N || (t->stride(d - 1) != 1 && x.N != 1) || (d == 2 && t->size(0) != x.B)) return false;
+    p = (const int*)t->data_ptr();
+    stride = d == 2 ? t->stride(0) : 0;
+    return true;
+}
+
+// (segments, document, order or None, cap, scale, workspace)
+PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Joint x;
+    const int *document, *order = nullptr;
+    long long document_stride, order_stride = 0;
+    float cap, scale;
+    if (n != 6 || !joint_segments(a[0], x) || !current(x.device) || !number(a[3], cap) || !number(a[4], scale)) Py_RETURN_NONE;
+    for (int i = 0; i < x.n; ++i)                      // (segments of different devices)
+        if (THPVariable_Unpack(PySequence_Fast_GET_ITEM(PySequence_Fast_GET_ITEM(a[0], i), 0)).get_device() != x.device) Py_RETURN_NONE;
+    if (!per_token(a[1], x, document, document_stride) || (a[2] != Py_None && !per_token(a[2], x, order, order_stride))) Py_RETURN_NONE;
+    const at::Tensor* t = plain(a[5]);
+    if (!t || !t->is_contiguous() || t->get_device() != x.device) Py_RETURN_NONE;
+    void* ws = t->data_ptr();
+    const size_t bytes = t->nbytes();
+    return launch(x.device, [&](void* s) {
+        return attn_packed(x.seg, x.n, x.B, x.H, x.D, document, document_stride, order, order_stride, cap, scale, ws, bytes, s);
+    });
+}
+
 // bind(address of each entry point, .., RopeAxis): of the library that binding.py has loaded
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long p[13];
+    unsigned long long p[18];
     PyTypeObject* axis;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKO!", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12], &PyType_Type, &axis)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKKKKKKO!", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12],
+                          &p[13], &p[14], &p[15], &p[16], &p[17], &PyType_Type, &axis)) return nullptr;
     attn_dense = (decltype(attn_dense))p[0];
     attn_block_sparse = (decltype(attn_block_sparse))p[1];
     attn_joint = (decltype(attn_joint))p[2];
@@ -527,6 +656,11 @@ PyObject* bind(PyObject*, PyObject* args)
     layer_table = (decltype(layer_table))p[10];
     layer_qk = (decltype(layer_qk))p[11];
     layer_rope = (decltype(layer_rope))p[12];
+    rows_quantize = (decltype(rows_quantize))p[13];
+    rows_modulate = (decltype(rows_modulate))p[14];
+    int8_linear = (decltype(int8_linear))p[15];
+    int8_linear_bytes = (decltype(int8_linear_bytes))p[16];
+    attn_packed = (decltype(attn_packed))p[17];
     Py_INCREF(axis);
     Py_XSETREF(axis_type, (PyObject*)axis);
     PyObject* c = PyImport_ImportModule("torch._C");
@@ -551,7 +685,8 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 #define NATIVE(f) {#f, (PyCFunction)(void (*)(void))guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, NATIVE(dense), NATIVE(block_sparse), NATIVE(select), NATIVE(joint),
                          NATIVE(joint_select), NATIVE(store), NATIVE(reuse), NATIVE(linear), NATIVE(modulate), NATIVE(table),
-                         NATIVE(qk_norm_rope), NATIVE(rope), {nullptr, nullptr, 0, nullptr}};
+                         NATIVE(qk_norm_rope), NATIVE(rope), NATIVE(quantize), NATIVE(modulate8), NATIVE(linear8),
+                         NATIVE(packed_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "native_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

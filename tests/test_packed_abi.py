@@ -155,3 +155,14 @@ def test_python_forms_take_tensors_of_the_gpu_alone():
             call()
     with pytest.raises(ValueError):
         ra.rapid_attn_packed([], torch.zeros(4, dtype=torch.int32))
+
+
+@pytest.mark.skipif(binding._load_native().__class__ is binding._NoNative, reason="the native calls are not built for this torch")
+def test_native_forms_leave_other_tensors_to_the_python_form():
+    x, q8, s = torch.zeros((1, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 4, 64), dtype=torch.int8), torch.zeros((1, 4))
+    q, d = torch.zeros((1, 2, 4, 64), dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    native = binding._load_native()
+    assert native.quantize(x, q8, s) is None and native.quantize(x) is None
+    assert native.modulate8(x, q8, s, None, None, 1e-6, None) is None
+    assert native.linear8(q8, s, q8[0], s[0], x, None, "none", None, None, None, None) is None
+    assert native.packed_attention([(q, q, q, q)], d, None, 0.0, 0.0, s) is None
