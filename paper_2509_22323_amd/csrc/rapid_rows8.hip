@@ -23,32 +23,41 @@ struct RowsParams {
     int x_sn, q_sn;
     int documents, M, n, C;
     float eps;
+    double share;            // 1 / C
 };
 
 __device__ __forceinline__ float low(unsigned pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(unsigned pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-template <class T>
-__device__ __forceinline__ T other(T v, int lane_xor)
+template <int CTRL>
+__device__ __forceinline__ unsigned moved(unsigned v)
 {
-    return __shfl_xor(v, lane_xor, 64);
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
-// The largest value of the wavefront, in every lane.
-template <class T>
-__device__ __forceinline__ T most_of_lanes(T v)
+template <int CTRL>
+__device__ __forceinline__ double moved(double v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const T w = other(v, d);
-        v = w > v ? w : v;
-    }
-    return v;
+    return __hiloint2double((int)moved<CTRL>((unsigned)__double2hiint(v)), (int)moved<CTRL>((unsigned)__double2loint(v)));
 }
-__device__ __forceinline__ double sum_of_lanes(double v)
+// f over the values of the wavefront, in every lane.
+template <class T, class F>
+__device__ __forceinline__ T over_lanes(T v, F f)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += other(v, d);
-    return v;
+    v = f(v, moved<0xB1>(v));                          // lane ^ 1
+    v = f(v, moved<0x4E>(v));                          // lane ^ 2
+    v = f(v, moved<0x141>(v));                         // 7 - lane of every 8
+    v = f(v, moved<0x140>(v));                         // 15 - lane of every 16
+    auto swapped = [&](auto swap) {
+        if constexpr (sizeof(T) == 8) {
+            const auto l = swap((unsigned)__double2loint(v)), h = swap((unsigned)__double2hiint(v));
+            return f(__hiloint2double((int)h[0], (int)l[0]), __hiloint2double((int)h[1], (int)l[1]));
+        } else {
+            const auto w = swap(v);
+            return f((T)w[0], (T)w[1]);
+        }
+    };
+    v = swapped([](unsigned w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+    return swapped([](unsigned w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
 }
 
 // v in every wavefront of a row -> f over them, in all of them
@@ -121,8 +130,8 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void quantize_rows_ke
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max(most, max(raw[c][i] & 0x7fff0000u, raw[c][i] << 17 >> 1));
-    most = most_of_lanes(most);
-    most = over_waves<WAVES>(most, part, wave, own, [](unsigned a, unsigned b) { return max(a, b); });
+    auto larger = [](unsigned a, unsigned b) { return max(a, b); };
+    most = over_waves<WAVES>(over_lanes(most, larger), part, wave, own, larger);
     if (!there) return;
     const bool plain = most < 0x7f800000u && most != 0u;
     const Divided d = divided_by(plain ? __uint_as_float(most) : 1.0f);
@@ -157,8 +166,8 @@ __global__ __launch_bounds__(512) void quantize_long_rows_kernel(RowsParams p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max(most, max(raw[i] & 0x7fff0000u, raw[i] << 17 >> 1));
     }
-    most = most_of_lanes(most);
-    most = over_waves<8>(most, part, threadIdx.x / 64, 0, [](unsigned a, unsigned b) { return max(a, b); });
+    auto larger = [](unsigned a, unsigned b) { return max(a, b); };
+    most = over_waves<8>(over_lanes(most, larger), part, threadIdx.x / 64, 0, larger);
     const bool plain = most < 0x7f800000u && most != 0u;
     const Divided d = divided_by(plain ? __uint_as_float(most) : 1.0f);
     signed char* q = p.q + b * p.q_sb + (long long)r * p.q_sn;
@@ -176,6 +185,28 @@ __global__ __launch_bounds__(512) void quantize_long_rows_kernel(RowsParams p)
         *(u32x2*)(q + at) = out;
     }
     if (threadIdx.x == 0) p.q_scale[m] = most > 0x7f7fffffu ? __uint_as_float(0x7fc00000u) : __uint_as_float(most) / 127.0f;
+}
+
+// 1 / v and 1 / sqrt(v) from the instructions' 2^-23 by two steps of Newton's, within some 2^-51.  (Divisions and a root to the last place
+// are half as many instructions again as the rest of a row of 1536.)
+__device__ __forceinline__ double one_by(double v)
+{
+    double r = __builtin_amdgcn_rcp(v);
+    r = __builtin_fma(__builtin_fma(-v, r, 1.0), r, r);
+    return __builtin_fma(__builtin_fma(-v, r, 1.0), r, r);
+}
+__device__ __forceinline__ double one_by_root(double v)
+{
+    double r = __builtin_amdgcn_rsq(v);
+    r = __builtin_fma(0.5 * r, __builtin_fma(-v * r, r, 1.0), r);
+    return __builtin_fma(0.5 * r, __builtin_fma(-v * r, r, 1.0), r);
+}
+// The larger of a and |b| (neither signals; a NaN is not taken).  Assembly: the compiler's form takes another instruction to quiet what cannot signal.
+__device__ __forceinline__ double larger_of(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, |%2|" : "=v"(r) : "v"(a), "v"(b));
+    return r;
 }
 
 // The norm, in fp64: what it ends in are whole numbers, and a result in 32 bits would be on another side of a border between two of them than
@@ -210,7 +241,10 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
             sum += (double)high(raw[c][i]);
         }
     auto add = [](double a, double b) { return a + b; };
-    const double mean = over_waves<WAVES>(sum_of_lanes(sum), part[0], wave, own, add) / (double)p.C;
+    auto larger = [](double a, double b) { return larger_of(a, b); };
+    // (the mean rounded once: that of equal elements is their value)
+    const double all = over_waves<WAVES>(over_lanes(sum, add), part[0], wave, own, add), near = all * p.share;
+    const double mean = __builtin_fma(__builtin_fma(-near, (double)p.C, all), p.share, near);
     double y[CHUNKS][8], square = 0.0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
@@ -221,8 +255,8 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
             square = __builtin_fma(y[c][i], y[c][i], square);
         }
     }
-    const double inv = 1.0 / sqrt(over_waves<WAVES>(sum_of_lanes(square), part[1], wave, own, add) / (double)p.C + (double)p.eps);
-    double most = 0.0, number = 0.0;                   // number: NaN where an element is none
+    const double inv = one_by_root(__builtin_fma(over_waves<WAVES>(over_lanes(square, add), part[1], wave, own, add), p.share, (double)p.eps));
+    double most = 0.0, number = inv * 0.0;             // number: NaN where an element is none
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int at = 8 * (c * LANES + lane);
@@ -240,16 +274,15 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            most = fmax(most, fabs(y[c][i]));
-            number = __builtin_fma(y[c][i], 0.0, number);
+            most = larger(most, y[c][i]);
+            if (p.scale) number = __builtin_fma(y[c][i], 0.0, number);
         }
     }
-    most = fmax(most, number != 0.0 ? INFINITY : 0.0);
-    most = most_of_lanes(most);
-    most = over_waves<WAVES>(most, part[2], wave, own, [](double a, double b) { return a > b ? a : b; });
+    most = larger(most, number != 0.0 ? INFINITY : 0.0);
+    most = over_waves<WAVES>(over_lanes(most, larger), part[2], wave, own, larger);
     if (!written) return;
     const bool plain = most < INFINITY && most > 0.0;
-    const double by = 127.0 / (plain ? most : 1.0);
+    const double by = 127.0 * one_by(plain ? most : 1.0);
     signed char* q = p.q + b * p.q_sb + (long long)r * p.q_sn;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
@@ -345,8 +378,10 @@ int rapid_norm_modulate_int8(const rapid_rows* x, const rapid_rows* q, float* q_
     p.document = document;
     p.documents = documents;
     p.eps = eps;
+    p.share = 1.0 / C;
     if (C <= 512) return launch_norm<1, 1>(p, stream);
     if (C <= 1024) return launch_norm<1, 2>(p, stream);
+    if (C <= 1536) return launch_norm<1, 3>(p, stream);
     if (C <= 2048) return launch_norm<1, 4>(p, stream);
     if (C <= 4096) return launch_norm<2, 4>(p, stream);
     if (C <= 8192) return launch_norm<4, 4>(p, stream);
