@@ -1,5 +1,6 @@
 """One joint layer of an MM-DiT on the library's operators (Sec. 3.1: image and text tokens in tensors of their own, each with
-weights of its own, joined for attention alone; every projection under the conditioning of the time step).
+weights of its own, joined for attention alone; every projection under the conditioning of the time step): in bf16 over a batch, or in
+8 bits over requests of any sizes packed into one sequence.
 
 Weights are the caller's (there are none here); buffers are made once, a run allocates nothing and can be captured into a graph.
 Inference only: runs are not recorded by autograd, whatever the weights require.
@@ -21,12 +22,12 @@ WEIGHTS = ("mod_w", "mod_b",           # [6C, C]: shift, scale, gate of the atte
 _NONE_ALLOWED = ("mod_b", "qkv_b", "q_norm", "k_norm", "out_b", "ff_in_b", "ff_out_b")
 
 
-def _check_sizes(weights, B, H, D, image, text, layout, eps):
+def _check_sizes(weights, B, H, D, image, text, layout, eps, tile=128, wide=8):
     """What a run would refuse half way through it."""
     if B < 1 or H < 1 or D not in (64, 128):
         raise ValueError(f"B = {B}, H = {H}, D = {D}: D is 64 or 128, B and H are at least 1")
-    if image < 128 or image % 128 != 0:
-        raise ValueError(f"{image} image tokens: their number must be a multiple of 128")
+    if image < tile or image % tile != 0:
+        raise ValueError(f"{image} image tokens: their number must be a multiple of {tile}")
     if text < 1:
         raise ValueError(f"{text} text tokens: there must be one at least")
     if layout not in _b.ROPE_LAYOUTS:
@@ -38,8 +39,8 @@ def _check_sizes(weights, B, H, D, image, text, layout, eps):
     C = H * D
     for stream, w in zip(("image", "text"), weights):
         F = w["ff_in_w"].shape[0]
-        if F < 8 or F % 8 != 0:
-            raise ValueError(f"{stream} stream: {F} channels of the feed-forward block, not a multiple of 8")
+        if F < wide or F % wide != 0:
+            raise ValueError(f"{stream} stream: {F} channels of the feed-forward block, not a multiple of {wide}")
         for name, shape in zip(WEIGHTS, ((6 * C, C), (6 * C,), (3 * C, C), (3 * C,), (D,), (D,), (C, C), (C,), (F, C), (F,), (C, F), (C,))):
             if w[name] is None and name in _NONE_ALLOWED:
                 continue
@@ -112,4 +113,100 @@ class JointLayer:
             _b.rapid_norm_modulate(x, h, mod[:, 4], mod[:, 3], self.eps)
             _b.rapid_linear(h, w["ff_in_w"], f, w["ff_in_b"], "gelu_tanh", workspace=self.workspace)
             _b.rapid_linear(f, w["ff_out_w"], x, w["ff_out_b"], "none", mod[:, 5], x, self.workspace)
+        return image, text
+
+
+class PackedLayer:
+    """The same layer in 8 bits over packed requests: the image tokens of all of them one after the other in one tensor, their texts in
+    another, each request (a document) under a conditioning vector of its own and seeing itself alone.  The projections are products of
+    8-bit integers with scales for each token and channel; what a token comes to does not depend on what it is packed with, but for
+    the order in which its attention's sums are added.
+
+    weights as JointLayer takes them; those of the projections are quantised here and not kept.  image, text: tokens that the
+    tensors of a run have, any numbers; documents: how many requests a run holds at most; axes (RopeAxis each): the rotation of
+    queries and keys, None = none.  F is a multiple of 16."""
+
+    PRODUCTS = ("qkv_w", "out_w", "ff_in_w", "ff_out_w")
+
+    def __init__(self, weights, H, D, image, text, documents, axes=None, layout="interleaved", eps=1e-6):
+        import torch
+        _check_sizes(weights, 1, H, D, image, text, layout, eps, 1, 16)
+        if documents < 1:
+            raise ValueError(f"{documents} documents: there must be one at least")
+        self.H, self.D, self.layout, self.eps, self.axes, self.documents = H, D, layout, eps, axes, documents
+        self.tokens = (image, text)
+        self.small = [{k: t for k, t in w.items() if k not in self.PRODUCTS} for w in weights]
+        device = weights[0]["qkv_w"].device
+        self.device = device.index
+        C, wide = H * D, [w["ff_in_w"].shape[0] for w in weights]
+
+        def empty(*shape, dtype=torch.bfloat16):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        def rows(n, width):                                # 8-bit rows and their scales (zeros: rows of no document stay as they are)
+            return torch.zeros((n, width), dtype=torch.int8, device=device), torch.zeros(n, dtype=torch.float32, device=device)
+
+        self.weights = [{k: _b.rapid_quantize_rows(w[k], empty(*w[k].shape, dtype=torch.int8), empty(w[k].shape[0], dtype=torch.float32))
+                         for k in self.PRODUCTS} for w in weights]
+        self.mod = [empty(documents, 6, C) for _ in weights]
+        self.h = [rows(n, C) for n in self.tokens]
+        self.qkv = [empty(1, n, 3, H, D) for n in self.tokens]
+        self.o = [empty(1, n, H, D) for n in self.tokens]
+        self.o8 = [rows(n, C) for n in self.tokens]
+        self.f = [empty(n, F) for n, F in zip(self.tokens, wide)]
+        self.f8 = [rows(n, F) for n, F in zip(self.tokens, wide)]
+        self.table = None if axes is None else empty(image + text, sum(int(a.dim) for a in axes) // 2, 2, dtype=torch.float32)
+        need = max(max(_b.rapid_linear_int8_workspace_bytes(M, N, K) for n, F in zip(self.tokens, wide)
+                       for M, N, K in ((n, 3 * C, C), (n, C, C), (n, F, C), (n, C, F))),
+                   max(_b.rapid_linear_workspace_bytes(m, 6 * C, C) for m in range(1, documents + 1)))
+        self.workspace = empty(max(need, 16), dtype=torch.uint8)
+        self.attention_workspace = empty(max(_b.rapid_attn_packed_workspace_bytes(1, H, image + text, D), 16), dtype=torch.uint8)
+        self.rows = [tuple(t.permute(2, 0, 3, 1, 4)) for t in self.qkv]            # (q, k, v) [1, H, n, D] of each stream
+        self.norms = [(w["q_norm"], w["k_norm"]) for w in weights]
+
+    def run(self, image, text, conditioning, document, positions=None, order=None, cap=0.0):
+        """image [n, C], text [m, C] <- the layer's output, in place; rows of no document stay as they are.  conditioning: [documents, C]
+        (as many as there are, at most those that the layer was made for); document: int32 [n + m], the request of every token of
+        image and then text, -1 for padding; positions: int32 [n + m, axes], needed where the layer has axes; order, cap as
+        rapid_attn_packed."""
+        if conditioning.dim() != 2 or not 1 <= conditioning.shape[0] <= self.documents:
+            raise ValueError(f"conditioning: {list(conditioning.shape)}, a vector each of 1 to {self.documents} documents")
+        if (positions is None) != (self.axes is None):
+            raise ValueError("positions: where the layer has axes, and only there")
+        for name, t in (("document", document), ("order", order)):
+            if t is not None and tuple(t.shape) != (sum(self.tokens),):
+                raise ValueError(f"{name} must be [{sum(self.tokens)}], not {list(t.shape)}")
+        if not 0 <= cap < float("inf"):
+            raise ValueError("cap must be finite and not negative")
+        import torch
+        if torch._C._cuda_getDevice() == self.device:
+            return self._run(image, text, conditioning, document, positions, order, cap)
+        with torch.cuda.device(self.device):
+            return self._run(image, text, conditioning, document, positions, order, cap)
+
+    def _run(self, image, text, conditioning, document, positions, order, cap):
+        hidden = (image, text)
+        n = self.tokens[0]
+        documents = (document[:n], document[n:])
+        mods = [mod[:conditioning.shape[0]] for mod in self.mod]
+        if positions is not None:
+            _b.rapid_rope_table(positions, self.axes, self.table)
+
+        def linear(of, w, name, bias, out, *rest, document=None):
+            _b.rapid_linear_int8(*of, *w[name], out, bias, *rest, document=document, workspace=self.workspace)
+
+        for x, h, mod, qkv, w, small, d in zip(hidden, self.h, mods, self.qkv, self.weights, self.small, documents):
+            _b.rapid_linear(conditioning, small["mod_w"], mod.view(mod.shape[0], -1), small["mod_b"], workspace=self.workspace)
+            _b.rapid_norm_modulate_int8(x, *h, mod[:, 1], mod[:, 0], self.eps, d)
+            linear(h, w, "qkv_w", small["qkv_b"], qkv.view(x.shape[0], -1))
+        _b.rapid_qk_norm_rope([(q, k, q, k) for q, k, _ in self.rows], self.norms, self.table, self.layout, self.eps)
+        _b.rapid_attn_packed([(q, k, v, o.transpose(1, 2)) for (q, k, v), o in zip(self.rows, self.o)], document, order, cap,
+                             workspace=self.attention_workspace)
+        for i, (x, h, mod, w, small, d) in enumerate(zip(hidden, self.h, mods, self.weights, self.small, documents)):
+            _b.rapid_quantize_rows(self.o[i].view(x.shape), *self.o8[i])
+            linear(self.o8[i], w, "out_w", small["out_b"], x, "none", mod[:, 2], x, document=d)
+            _b.rapid_norm_modulate_int8(x, *h, mod[:, 4], mod[:, 3], self.eps, d)
+            linear(h, w, "ff_in_w", small["ff_in_b"], self.f[i], "gelu_tanh")
+            _b.rapid_quantize_rows(self.f[i], *self.f8[i])
+            linear(self.f8[i], w, "ff_out_w", small["ff_out_b"], x, "none", mod[:, 5], x, document=d)
         return image, text
