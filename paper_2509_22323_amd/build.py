@@ -12,7 +12,7 @@ SOURCES = [os.path.join(HERE, "csrc", "rapid_attn.hip"), os.path.join(HERE, "csr
            os.path.join(HERE, "csrc", "rapid_mask.hip"),
            os.path.join(HERE, "csrc", "rapid_linear.hip"), os.path.join(HERE, "csrc", "rapid_layer.hip"),
            os.path.join(HERE, "csrc", "rapid_rows8.hip"), os.path.join(HERE, "csrc", "rapid_linear8.hip"),
-           os.path.join(HERE, "csrc", "rapid_attn_packed.hip")]
+           os.path.join(HERE, "csrc", "rapid_packed.hip")]
 OUT = os.path.join(HERE, "librapid_attn.so")
 # measurement aid used by bench.py only (an MFMA-only loop), kept out of the attention library
 PROBE_SOURCES = [os.path.join(HERE, "csrc", "mfma_probe.hip")]

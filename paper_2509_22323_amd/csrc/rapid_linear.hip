@@ -15,12 +15,6 @@
 
 namespace {
 
-template <int WR, int FN, bool SPLIT>
-__global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(LinearParams p, int items)
-{
-    wide_tiles<WR, FN, SPLIT>(p, items);
-}
-
 // The sums of a product's pieces, in their order, and the epilogue: eight outputs a lane.
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
 {
@@ -153,7 +147,7 @@ int launch_wide(const LinearParams& p, void* stream)
     const long long items = (((long long)p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * (SPLIT ? p.pieces : 1);
     if (items >= (1LL << 31) - 4096) return RAPID_ERR_SHAPE;
     const long long most = CUS * (4 / WR);
-    hipLaunchKernelGGL((linear_wide_kernel<WR, FN, SPLIT>), dim3((unsigned)(items < most ? items : most)), dim3(WR * 128), 0,
+    hipLaunchKernelGGL((linear_wide_kernel<WR, FN, SPLIT, LinearParams>), dim3((unsigned)(items < most ? items : most)), dim3(WR * 128), 0,
                        (hipStream_t)stream, p, (int)items);
     if constexpr (SPLIT) {
         const long long lanes = (long long)p.M * (p.pitch / 8);

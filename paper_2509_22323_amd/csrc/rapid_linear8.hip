@@ -11,12 +11,6 @@
 
 namespace {
 
-template <int WR, int FN, bool SPLIT>
-__global__ __launch_bounds__(WR * 128, 2) void linear8_wide_kernel(Linear8Params p, int items)
-{
-    wide_tiles<WR, FN, SPLIT>(p, items);
-}
-
 // The row of the gate that row m takes (sample b); below 0: the row is not written.
 __device__ __forceinline__ int vector_of(const Linear8Params& p, int m, int b)
 {
@@ -171,7 +165,7 @@ int launch_wide(const Linear8Params& p, void* stream)
     const long long items = (((long long)p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN) * (SPLIT ? p.pieces : 1);
     if (items >= (1LL << 31) - 4096) return RAPID_ERR_SHAPE;
     const long long most = CUS * (4 / WR);
-    hipLaunchKernelGGL((linear8_wide_kernel<WR, FN, SPLIT>), dim3((unsigned)(items < most ? items : most)), dim3(WR * 128), 0,
+    hipLaunchKernelGGL((linear_wide_kernel<WR, FN, SPLIT, Linear8Params>), dim3((unsigned)(items < most ? items : most)), dim3(WR * 128), 0,
                        (hipStream_t)stream, p, (int)items);
     if constexpr (SPLIT) {
         const long long lanes = (long long)p.M * (p.pitch / 8);

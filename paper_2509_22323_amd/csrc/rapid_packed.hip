@@ -274,7 +274,7 @@ struct Visit {
 };
 
 template <int D, bool CAP>
-__global__ __launch_bounds__(WAVES * 64, 2) void attn_packed_kernel(PackedParams p)
+__global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParams p)
 {
     typedef Lds<D> L;
     constexpr int KS = D / 32, DT = D / 16;
@@ -751,8 +751,8 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
         hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 3) / 4), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
     }
     const dim3 grid(8u * (unsigned)(pairs / 8 * per + (pairs % 8 * per + 7) / 8));
-    auto kernel = D == 64 ? cap > 0.f ? attn_packed_kernel<64, true> : attn_packed_kernel<64, false>
-                          : cap > 0.f ? attn_packed_kernel<128, true> : attn_packed_kernel<128, false>;
+    auto kernel = D == 64 ? cap > 0.f ? packed_tiles_kernel<64, true> : packed_tiles_kernel<64, false>
+                          : cap > 0.f ? packed_tiles_kernel<128, true> : packed_tiles_kernel<128, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(WAVES * 64), 0, (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? RAPID_OK : RAPID_ERR_DEVICE;
 }

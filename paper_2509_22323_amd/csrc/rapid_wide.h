@@ -84,7 +84,7 @@ constexpr int STEP = ROW / (int)sizeof(T);             // inputs per step
 constexpr int MOST_PIECES = 8;                         // along K
 
 template <int WR, int FN, bool SPLIT, class P>
-__device__ __forceinline__ void wide_tiles(P p, int items)
+__global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(P p, int items)
 {
     typedef typename P::Type T;
     constexpr bool WHOLES = std::is_same_v<T, signed char>;           // products of whole numbers: sums in 32 bits, scales behind them
@@ -386,25 +386,27 @@ __device__ __forceinline__ void wide_tiles(P p, int items)
             constexpr int MOST_AHEAD = EVEN ? FN == 8 ? (WHOLES ? 2 : 4) : 6 : FN == 8 ? 1 : 3, AHEAD = ALL < MOST_AHEAD ? ALL : MOST_AHEAD;
             bf16x8 gate[SIDE + 1] = {};
             Eight residuals[AHEAD] = {}, gates[SINGLE ? 1 : AHEAD] = {};
-            // of whole numbers: the scales and documents of this lane's rows, and the scales and bias of a column of units, the next one under way
+            // of whole numbers: the scales and documents of this lane's rows, and the scales and bias of a column of units, the next one under
+            // way where there are registers for it
+            constexpr int HELD = FN == 8 ? 1 : 2;
             constexpr int MINE = WHOLES ? FM + FN % 2 * FM / 2 : 1;
             float x_scale[MINE] = {};
             int document[MINE] = {};
-            f32x4 w_scale[2][2] = {};
-            bf16x8 added[2] = {};
+            f32x4 w_scale[HELD][2] = {};
+            bf16x8 added[HELD] = {};
             auto of_row = [](int u) { return u < UNITS ? u % FM : FM + u - UNITS; };
             auto load_column = [&](const auto& p, int c) {
                 const int n = column(c < SIDE ? c * FM : UNITS);
                 if (n >= p.N) return;
                 if (WHOLE || n + 8 <= p.N) {
                     typedef f32x4 f32x4_anywhere __attribute__((aligned(4)));
-                    w_scale[c % 2][0] = *(const f32x4_anywhere*)(p.w_scale + n);
-                    w_scale[c % 2][1] = *(const f32x4_anywhere*)(p.w_scale + n + 4);
+                    w_scale[c % HELD][0] = *(const f32x4_anywhere*)(p.w_scale + n);
+                    w_scale[c % HELD][1] = *(const f32x4_anywhere*)(p.w_scale + n + 4);
                 } else {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) w_scale[c % 2][q / 4][q % 4] = p.w_scale[min(n + q, p.N - 1)];
+                    for (int q = 0; q < 8; ++q) w_scale[c % HELD][q / 4][q % 4] = p.w_scale[min(n + q, p.N - 1)];
                 }
-                if (p.bias) added[c % 2] = eight_of(p.bias, n, p.N, p.even);
+                if (p.bias) added[c % HELD] = eight_of(p.bias, n, p.N, p.even);
             };
             if constexpr (WHOLES) {
 #pragma unroll
@@ -416,7 +418,7 @@ __device__ __forceinline__ void wide_tiles(P p, int items)
                 load_column(p, 0);
             }
             // where the gate of row m begins, and whether the row is written
-            auto gate_of = [&](const auto& p, int u, int m) {
+            [[maybe_unused]] auto gate_of = [&](const auto& p, int u, int m) {
                 if constexpr (WHOLES && !SINGLE) {
                     if (p.document) {
                         const int d = document[of_row(u)];
@@ -425,7 +427,7 @@ __device__ __forceinline__ void wide_tiles(P p, int items)
                 }
                 return of(m, p.gate, p.g_sb, 0);
             };
-            auto written = [&](const auto& p, int u) {
+            [[maybe_unused]] auto written = [&](const auto& p, int u) {
                 if constexpr (WHOLES && !SINGLE) return !p.document || (unsigned)document[of_row(u)] < (unsigned)p.documents;
                 else return true;
             };
@@ -433,7 +435,9 @@ __device__ __forceinline__ void wide_tiles(P p, int items)
                 const int m = row(u), n = column(u);
                 if (m >= p.M || n >= p.N) return;
                 if (p.residual) residuals[u % AHEAD] = load(of(m, p.residual, p.r_sb, p.r_sn), n);
-                if (!SINGLE && p.gate && !one_sample) gates[u % AHEAD] = load(gate_of(p, u, m), n);
+                if constexpr (WHOLES) {
+                    if (!SINGLE && p.gate && !one_sample) gates[u % AHEAD] = load(gate_of(p, u, m), n);
+                } else if (!SINGLE && p.gate && !one_sample) gates[u % AHEAD] = load(of(m, p.gate, p.g_sb, 0), n);
             };
             if constexpr (!BARE) {
                 if (p.gate && one_sample) {
@@ -454,16 +458,17 @@ __device__ __forceinline__ void wide_tiles(P p, int items)
                 if constexpr (WHOLES) {
                     const float by = x_scale[of_row(u)];
                     const int c = u < UNITS ? across(u) : SIDE;
-                    if (u % FM == 0 && u < UNITS && c + 1 < SIDE + FN % 2) load_column(p, c + 1);
+                    if (HELD == 2 && u % FM == 0 && u < UNITS && c + 1 < SIDE + FN % 2) load_column(p, c + 1);
+                    if (HELD == 1 && u % FM == 0 && c > 0) load_column(p, c);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         auto both = __builtin_amdgcn_permlane16_swap(a[q], b[q], false, false);
-                        z[q] = (float)(int)both[0] * by * w_scale[c % 2][0][q];
-                        z[4 + q] = (float)(int)both[1] * by * w_scale[c % 2][1][q];
+                        z[q] = (float)(int)both[0] * by * w_scale[c % HELD][0][q];
+                        z[4 + q] = (float)(int)both[1] * by * w_scale[c % HELD][1][q];
                     }
                     if (p.bias) {
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) z[q] += (float)added[c % 2][q];
+                        for (int q = 0; q < 8; ++q) z[q] += (float)added[c % HELD][q];
                     }
                 } else {
 #pragma unroll
@@ -482,12 +487,16 @@ __device__ __forceinline__ void wide_tiles(P p, int items)
                     bf16x8 by = gate[u < UNITS ? across(u) : SIDE];
                     bf16x8 residual = {};
                     if (p.residual) residual = value(residuals[u % AHEAD], of(m, p.residual, p.r_sb, p.r_sn), n);
-                    if (!SINGLE && p.gate && !one_sample) by = value(gates[u % AHEAD], gate_of(p, u, m), n);
+                    if constexpr (WHOLES) {
+                        if (!SINGLE && p.gate && !one_sample) by = value(gates[u % AHEAD], gate_of(p, u, m), n);
+                    } else if (!SINGLE && p.gate && !one_sample) by = value(gates[u % AHEAD], of(m, p.gate, p.g_sb, 0), n);
                     out = finished(p, z, by, residual);
                     if (u + AHEAD < ALL) load_ahead(u + AHEAD);
                 }
                 if (u == ALL / 2 && more) load_bias();     // (half of the sums' registers are free)
-                if (m < p.M && n < p.N && written(p, u)) {
+                if constexpr (WHOLES)
+                    if (!written(p, u)) continue;
+                if (m < p.M && n < p.N) {
                     __bf16* y = (__bf16*)of(m, p.y, p.y_sb, p.y_sn);
                     if constexpr (EVEN) *(bf16x8_anywhere*)(y + n) = out;
                     else if constexpr (WHOLE) store(y + n, out, false);
