@@ -193,6 +193,8 @@ __device__ __forceinline__ Known known_of_group(const PackedParams& p, const Kno
     return mine;
 }
 
+constexpr int FEW = 16;                                // tiles that every workgroup looks at itself
+
 // What is known of all tiles, and the groups of a sample in the order of what they have to do, most first: workgroups go to the CUs in
 // turn as these get free, so that what is left for last is short.  A workgroup a sample, of PLANNED tiles at most.
 constexpr int PLANNED = 1026;
@@ -246,6 +248,9 @@ struct Lds {
     // 16-byte chunks of a row change places by row, so that the 16 rows (K) or 4 x 16 patches (V) that are read at a time lie in different banks
     static __device__ __forceinline__ int turn_k(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
     static __device__ __forceinline__ int turn_v(int row) { return D == 128 ? (row & 7) << 1 : (row >> 1 & 3) << 1; }
+    // what PER j rows on change of a chunk's place in bytes, for rows PER j + 0 .. PER - 1 of 16
+    static constexpr unsigned next_k(int j) { return 64u * j; }
+    static constexpr unsigned next_v(int j) { return D == 128 ? 128u * (j & 1) : 0u; }
 };
 
 // 1 KB from 64 lanes' offsets into LDS; 5 wait states behind a vector instruction that wrote the descriptor, one behind the write of M0
@@ -274,7 +279,7 @@ struct Visit {
 };
 
 template <int D, bool CAP>
-__global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParams p)
+__global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kernel(PackedParams p)
 {
     typedef Lds<D> L;
     constexpr int KS = D / 32, DT = D / 16;
@@ -282,6 +287,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
     __shared__ __align__(1024) char lds[4 * L::BYTES + 4 * TILE * 4];
     __shared__ __align__(16) Visit list[LIST];
     __shared__ int found[WAVES];
+    __shared__ int mine_doc[ROWS], mine_turn[ROWS];    // of the queries
+    __shared__ Known own_known[FEW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
 
     // Which rows: 8 heads at a time, an XCD each, so that an L2 holds the keys and values of few of them; of these the groups with most to
@@ -305,38 +312,47 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
     const bool second = group >= p.groups0;
     const Side& own = p.side[second];
     const int length = second ? p.N - p.n0 : p.n0, row0 = (second ? group - p.groups0 : group) * ROWS;
-    const Known* known = p.known + (long long)b * p.tiles;
-    const Known mine = known_of_group(p, known, group);
+    const Known* const known = p.known + (long long)b * p.tiles;
+    if (!p.known) {                                    // few tiles: every workgroup looks at them itself, which is faster than a launch before it
+        for (int tile = wave; tile < p.tiles; tile += WAVES) {
+            const Known k = known_of(p, b, tile, lane);
+            if (lane == 0) own_known[tile] = k;
+        }
+        __syncthreads();
+    }
+    const Known mine = p.known ? known_of_group(p, known, group) : known_of_group(p, own_known, group);
 
     // queries: lane (n, g) holds elements 32 t + 8 g .. + 7 of query 16 q + n
     const int q0 = row0 + 32 * wave;
     bf16x8 qf[2][KS];
-    int doc[2], turn[2];
     const long long at_in = b * own.in_sb + h * own.in_sh;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const int row = min(q0 + 16 * q + n, length - 1), t = row + (second ? p.n0 : 0);
+        const int row = min(q0 + 16 * q + n, length - 1);
         const char* from = own.q + at_in + (long long)row * own.in_sn + 16 * g;
 #pragma unroll
         for (int k = 0; k < KS; ++k) qf[q][k] = *(const bf16x8*)(from + 64 * k);
-        doc[q] = p.document[b * p.document_sb + t];
-        turn[q] = p.order ? p.order[b * p.order_sb + t] : 0;
+    }
+    if (tid < ROWS) {
+        const int t = min(row0 + tid, length - 1) + (second ? p.n0 : 0);
+        mine_doc[tid] = p.document[b * p.document_sb + t];
+        mine_turn[tid] = p.order ? p.order[b * p.order_sb + t] : 0;
     }
 
     // copies of a tile: this lane's rows and chunks
     const unsigned lds_at = (unsigned)(size_t)(lds_char*)lds;
     const unsigned crow = wave * L::COPIES * L::PER + lane / (64 / L::PER);
-    unsigned ck[L::COPIES], cv[L::COPIES];
-#pragma unroll
-    for (int j = 0; j < L::COPIES; ++j) {
-        const int row = crow + j * L::PER, c = lane % (64 / L::PER);
-        ck[j] = 16u * (c ^ L::turn_k(row));
-        cv[j] = 16u * (c ^ L::turn_v(row));
-    }
+    const int cchunk = lane % (64 / L::PER);
+    const unsigned ck = 16u * (cchunk ^ L::turn_k(crow)), cv = 16u * (cchunk ^ L::turn_v(crow));      // of the first copy; the others' differ by L::next_k, next_v
     const unsigned stride0 = p.side[0].in_sn, stride1 = p.side[1].in_sn;
     const long long delta0 = p.side[0].v - p.side[0].k, delta1 = p.side[1].v - p.side[1].k;
     const int* const documents = p.document + b * p.document_sb;
     const int* const orders = p.order ? p.order + b * p.order_sb : nullptr;
+    // a value such that nothing made from it is kept in registers over the loop
+    auto here = [](auto v) {
+        asm volatile("" : "+v"(v));
+        return v;
+    };
     auto copy = [&](const Visit& e, auto is_v, auto slot) {
         constexpr bool V = is_v.value;
         const bool s = (e.high >> 30 & 1) != 0;
@@ -344,10 +360,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
         unsigned long long base = (unsigned long long)(e.high & 0xffffu) << 32 | e.low;
         if constexpr (V) base += (unsigned long long)(s ? delta1 : delta0);
         const i32x4 buffer = {(int)(unsigned)base, (int)((unsigned)(base >> 32) & 0xffffu), e.bytes, 0x00020000};
-        const unsigned at = __umul24(crow, sn);
+        const unsigned at = __umul24(crow, sn), chunk = here(V ? cv : ck);
 #pragma unroll
         for (int j = 0; j < L::COPIES; ++j) {
-            const unsigned off = at + (unsigned)(j * L::PER) * sn + (V ? cv[j] : ck[j]);
+            const unsigned off = at + (unsigned)(j * L::PER) * sn + (chunk ^ (V ? L::next_v(j) : L::next_k(j)));
             const unsigned dst = lds_at + slot.value * L::BYTES + (wave * L::COPIES + j) * 1024;
             if (j == 0) copy_1k<true>(buffer, off, dst);
             else copy_1k<false>(buffer, off, dst);
@@ -355,8 +371,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
         if constexpr (V) {                             // with the documents and orders of its tokens, 4 bytes a lane
             if ((int)e.high < 0 && wave < 2 && (wave == 0 || orders)) {
                 const unsigned long long from = (unsigned long long)((wave == 0 ? documents : orders) + (e.token & 0xffffff));
-                const i32x4 words = {(int)(unsigned)from, (int)((unsigned)(from >> 32) & 0xffffu), 4 * ((e.token >> 24) + 1), 0x00020000};
-                const unsigned dst = lds_at + 4 * L::BYTES + (2 * (slot.value - 2) + wave) * 4 * TILE, off = 4u * lane;
+                const i32x4 words = {__builtin_amdgcn_readfirstlane((int)(unsigned)from), __builtin_amdgcn_readfirstlane((int)((unsigned)(from >> 32) & 0xffffu)),
+                                     __builtin_amdgcn_readfirstlane(4 * ((e.token >> 24) + 1)), 0x00020000};
+                const unsigned dst = lds_at + 4 * L::BYTES + (2 * (slot.value - 2) + wave) * 4 * TILE, off = 4u * here(lane);
                 asm volatile("s_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"{m0}"(dst), "v"(off), "s"(words));
             }
         }
@@ -370,13 +387,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
 #pragma unroll
     for (int d = 0; d < DT; ++d) vat[d] = vrow * L::RB + (((2 * d + ((n & 3) >> 1)) ^ L::turn_v(vrow)) << 4) + (n & 1) * 8;
 
-    f32x4 acc[DT][2] = {}, sums[2] = {};
+    f32x4 acc[DT][2] = {};
+    float sums[2] = {};                                // of this lane's weights
     float m[2] = {-1e30f, -1e30f};
     bool partly = false;
-    bf16x8 ones;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-
     typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
     typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
@@ -399,7 +413,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
         }
     };
     auto mask = [&](const Visit& e, auto slot, f32x4 (&s)[4][2]) {
+        const int lane_ = here(lane), n = lane_ & 15, g = lane_ >> 4;
         lds_char* const at = (lds_char*)lds + 4 * L::BYTES + 2 * slot.value * 4 * TILE + 16 * g;
+        const int doc[2] = {mine_doc[32 * wave + n], mine_doc[32 * wave + 16 + n]}, turn[2] = {mine_turn[32 * wave + n], mine_turn[32 * wave + 16 + n]};
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
             const i32x4 d = *(lds_i32x4*)(at + 64 * kt);
@@ -450,6 +466,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
     // AHEAD items before, and the matrix instructions of both groups of queries; behind each a quarter or two of the work on a pair of weights.
     auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], auto turn_) {
         constexpr int T = turn_.value;                 // K of this tile in slot T, V in slot 2 + T
+        // (a bound on a capped tile's scores is at hand with the choice of its formula, so their maximum is looked for only where that is too large)
+        bool look = true;
         if constexpr (CAP) {                           // (before the mask: what is hidden is not -cap)
             float size = 0.f;
 #pragma unroll
@@ -466,8 +484,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[kt][q][r] *= series(p, s[kt][q][r]);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) most[q] *= series(p, most[q]);
+                size *= series(p, size);
             } else {
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
@@ -475,13 +492,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) most[q] = exponent(most[q], scale, cap);
+                size = cap;
             }
+            look = __builtin_amdgcn_ballot_w64(size > fminf(m[0], m[1]) + 8.f) != 0ull;
         }
         if ((int)e.high < 0) {
             mask(e, turn_, s);
             partly = true;
+        }
+        if ((int)e.high < 0 || (CAP && look)) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) most[q] = largest(s, q);
         }
@@ -489,7 +508,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
 #pragma unroll
         for (int q = 0; q < 2; ++q)
             if constexpr (!CAP) most[q] *= scale;
-        if (__builtin_amdgcn_ballot_w64(most[0] > m[0] + 8.f || most[1] > m[1] + 8.f) != 0ull) {
+        if (look && __builtin_amdgcn_ballot_w64(most[0] > m[0] + 8.f || most[1] > m[1] + 8.f) != 0ull) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 float top = fmaxf(most[q], __shfl_xor(most[q], 16, 64));
@@ -504,7 +523,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
         }
         // Items 0 .. QK - 1: scores of the next tile (behind the last one: of what is there, which nobody looks at); QK .. : of 32 keys each,
         // what the weights add.  Pairs of weights 0 .. 7 of the first 32 keys, 8 .. 15 of the others, each before the items that take them.
-        constexpr int QK = 4 * KS, PV = DT, ALL = QK + 2 * PV, AHEAD = 3, EARLY = 40;
+        constexpr int QK = 4 * KS, PV = DT, ALL = QK + 2 * PV, AHEAD = D == 64 ? 1 : 3, EARLY = 40;
         bf16x8 f[AHEAD + 1];
         unsigned w[2][2][4];
         float x0, x1, e0, e1;
@@ -531,7 +550,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
                 e1 = __builtin_amdgcn_exp2f(x1);
             } else {
                 const bf16x2 both = {(__bf16)e0, (__bf16)e1};
+                const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
                 w[half][q][i] = __builtin_bit_cast(unsigned, both);
+                sums[q] = __builtin_amdgcn_fdot2_f32_bf16(both, ones, sums[q], false);
             }
         };
         constexpr std::integral_constant<int, 0> begin;
@@ -549,14 +570,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
                     constexpr int d = (I - QK) % PV;
                     const bf16x8 by = __builtin_bit_cast(bf16x8, w[half][q]);
                     acc[d][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[I % (AHEAD + 1)], by, acc[d][q], 0, 0, 0);
-                    if constexpr (d == PV - 1) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, by, sums[q], 0, 0, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 constexpr int M = 2 * QK, H = 2 * PV;
                 constexpr int from = at < M ? at * EARLY / M : at < M + H ? EARLY + (at - M) * (64 - EARLY) / H : 64;
                 constexpr int upto = at < M ? (at + 1) * EARLY / M : at < M + H ? EARLY + (at + 1 - M) * (64 - EARLY) / H : 64;
                 each(std::integral_constant<int, from>(), std::integral_constant<int, upto>(), quarter);
-                if constexpr (I == ALL - 2) most[q] = largest(next, q);
+                if constexpr (!CAP && I == ALL - 2) most[q] = largest(next, q);
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
@@ -568,8 +588,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
         const int upto = min(tiles - from, LIST);
         int count = 0;
         for (int i = 0; i < upto; i += WAVES * 64) {
-            const int tile = from + i + tid;
-            const int how = i + tid < upto ? sees(mine, known[tile]) : NONE;
+            const int at = i + here(tid), tile = from + at, how = at < upto ? sees(mine, p.known ? known[tile] : own_known[tile % FEW]) : NONE;
             const unsigned long long some = __builtin_amdgcn_ballot_w64(how != NONE);
             __syncthreads();
             if (lane == 0) found[wave] = __popcll(some);
@@ -642,34 +661,40 @@ __global__ __launch_bounds__(WAVES * 64, 2) void packed_tiles_kernel(PackedParam
     }
 
     // Results.  A weight of 0 times an infinity or NaN in a tile that not every query sees whole is NaN: such rows again, key by key.
+    const int lane_ = here(lane), n_ = lane_ & 15, g_ = lane_ >> 4;
     unsigned again = 0;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const int row = q0 + 16 * q + n;
-        const float inverse = 1.f / sums[q][0];
+        const int row = q0 + 16 * q + n_;
+        const bool some = mine_doc[32 * wave + 16 * q + n_] >= 0;
+        float sum = sums[q] + __shfl_xor(sums[q], 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        const float inverse = 1.f / sum;
         float all = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 4; ++r) all = __builtin_fmaf(acc[d][q][r], 0.f, all);
-        const unsigned long long bad = partly ? __builtin_amdgcn_ballot_w64(all != 0.f && row < length && doc[q] >= 0) : 0ull;
+        const unsigned long long bad = partly ? __builtin_amdgcn_ballot_w64(all != 0.f && row < length && some) : 0ull;
         const unsigned rows = (unsigned)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu;
         again |= rows << (16 * q);
-        if (row >= length || (rows >> n & 1) != 0) continue;
-        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * g;
+        if (row >= length || (rows >> n_ & 1) != 0) continue;
+        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * g_;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             bf16x4v out;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) out[r] = (__bf16)(doc[q] >= 0 ? acc[d][q][r] * inverse : 0.f);
+            for (int r = 0; r < 4; ++r) out[r] = (__bf16)(some ? acc[d][q][r] * inverse : 0.f);
             *(bf16x4v*)(o + 32 * d) = out;
         }
     }
     again = __builtin_amdgcn_readfirstlane(again);
     while (again != 0) {
+        int sample = b;                                // (its addresses are not to be kept over the loop above)
+        asm volatile("" : "+s"(sample));
         const int i = __builtin_ctz(again);
         again &= again - 1;
-        row_by_keys<D>(p, b, h, q0 + i + (second ? p.n0 : 0), lane);
+        row_by_keys<D>(p, sample, h, q0 + i + (second ? p.n0 : 0), lane_);
     }
 }
 
@@ -742,9 +767,10 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     p.tiles = p.tiles0 + (n1 + TILE - 1) / TILE;
     p.groups0 = (p.n0 + ROWS - 1) / ROWS;
     p.groups1 = (n1 + ROWS - 1) / ROWS;
-    p.known = (Known*)workspace;
     const int per = p.groups0 + p.groups1, pairs = B * H;
-    if (p.tiles <= PLANNED) {
+    p.known = p.tiles <= FEW ? nullptr : (Known*)workspace;
+    if (!p.known) {
+    } else if (p.tiles <= PLANNED) {
         p.sorted = (int*)(p.known + (size_t)B * p.tiles);
         hipLaunchKernelGGL(packed_plan_kernel, dim3((unsigned)B), dim3(1024), 0, (hipStream_t)stream, p);
     } else {
