@@ -12,6 +12,7 @@
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -34,6 +35,8 @@ struct PackedParams {
     int tiles0, tiles, groups0, groups1;               // tiles of the first segment, of both; groups of 128 queries of each
     Known* known;                                      // [B, tiles]
     int* sorted;                                       // [B, groups], most work first, or null
+    int pieces;                                        // of what a group has to do
+    float* partial;                                    // [B, H, groups, pieces]: what a piece comes to
     float scale;                                       // of a score: capped / log2(e), else as exponent of 2
     float cap;                                         // as exponent of 2; 0: none
     float small, series[5];                            // of a capped score: see series()
@@ -278,6 +281,12 @@ struct Visit {
     int token;                                         // its first one in the joint sequence, and (rows - 1) << 24
 };
 
+// What a piece of a group leaves: [ROWS, D], and a number each for the rows
+template <int D>
+struct Part {
+    static constexpr int SUM = ROWS * D, REFERENCE = SUM + ROWS, FLOATS = REFERENCE + ROWS;
+};
+
 template <int D, bool CAP>
 __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kernel(PackedParams p)
 {
@@ -294,7 +303,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
     // Which rows: 8 heads at a time, an XCD each, so that an L2 holds the keys and values of few of them; of these the groups with most to
     // do first; the heads that are left over are dealt out to all XCDs.
     const int per = p.groups0 + p.groups1, pairs = p.B * p.H, whole = pairs / 8, rest = pairs % 8;
-    const int xcd = blockIdx.x % 8, turn_in = blockIdx.x / 8;
+    const int piece = blockIdx.x / 8 % p.pieces, xcd = blockIdx.x % 8, turn_in = blockIdx.x / 8 / p.pieces;
     int head, rank;
     if (turn_in < whole * per) {
         rank = turn_in / whole;
@@ -391,7 +400,6 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
     float sums[2] = {};                                // of this lane's weights
     float m[2] = {-1e30f, -1e30f};
     bool partly = false;
-    typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
     typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
     typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -610,10 +618,11 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
             }
         }
         __syncthreads();
-        count = __builtin_amdgcn_readfirstlane(count);
+        const int first = count * piece / p.pieces;
+        count = __builtin_amdgcn_readfirstlane(count * (piece + 1) / p.pieces - first);
         if (count == 0) continue;
         auto visit = [&](int i) {
-            const Visit e = list[i];
+            const Visit e = list[first + i];
             return Visit{(unsigned)__builtin_amdgcn_readfirstlane(e.low), (unsigned)__builtin_amdgcn_readfirstlane(e.high),
                          __builtin_amdgcn_readfirstlane(e.bytes), __builtin_amdgcn_readfirstlane(e.token)};
         };
@@ -660,16 +669,36 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         arrive();                                      // before the list and the slots serve the next tiles
     }
 
+    const int lane_here = here(lane), n_here = lane_here & 15, g_here = lane_here >> 4;
+    float sum[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        sum[q] = sums[q] + __shfl_xor(sums[q], 16, 64);
+        sum[q] += __shfl_xor(sum[q], 32, 64);
+    }
+    if (p.pieces > 1) {                                // this piece's part: sums of V under the weights, of the weights, and their reference
+        typedef Part<D> P;
+        float* const part = p.partial + (((long long)head * per + group) * p.pieces + piece) * P::FLOATS;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int row = 32 * wave + 16 * q + n_here;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) *(f32x4*)(part + row * D + 16 * d + 4 * g_here) = acc[d][q];
+            if (g_here == 0) {
+                part[P::SUM + row] = sum[q];
+                part[P::REFERENCE + row] = m[q];
+            }
+        }
+        return;
+    }
+
     // Results.  A weight of 0 times an infinity or NaN in a tile that not every query sees whole is NaN: such rows again, key by key.
-    const int lane_ = here(lane), n_ = lane_ & 15, g_ = lane_ >> 4;
     unsigned again = 0;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const int row = q0 + 16 * q + n_;
-        const bool some = mine_doc[32 * wave + 16 * q + n_] >= 0;
-        float sum = sums[q] + __shfl_xor(sums[q], 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        const float inverse = 1.f / sum;
+        const int row = q0 + 16 * q + n_here;
+        const bool some = mine_doc[32 * wave + 16 * q + n_here] >= 0;
+        const float inverse = 1.f / sum[q];
         float all = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -678,14 +707,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         const unsigned long long bad = partly ? __builtin_amdgcn_ballot_w64(all != 0.f && row < length && some) : 0ull;
         const unsigned rows = (unsigned)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu;
         again |= rows << (16 * q);
-        if (row >= length || (rows >> n_ & 1) != 0) continue;
-        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * g_;
+        if (row >= length || (rows >> n_here & 1) != 0) continue;
+        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * g_here;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-            bf16x4v out;
+            bf16x4 out;
 #pragma unroll
             for (int r = 0; r < 4; ++r) out[r] = (__bf16)(some ? acc[d][q][r] * inverse : 0.f);
-            *(bf16x4v*)(o + 32 * d) = out;
+            *(bf16x4*)(o + 32 * d) = out;
         }
     }
     again = __builtin_amdgcn_readfirstlane(again);
@@ -694,8 +723,79 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         asm volatile("" : "+s"(sample));
         const int i = __builtin_ctz(again);
         again &= again - 1;
-        row_by_keys<D>(p, sample, h, q0 + i + (second ? p.n0 : 0), lane_);
+        row_by_keys<D>(p, sample, h, q0 + i + (second ? p.n0 : 0), lane_here);
     }
+}
+
+// The pieces of the groups' rows in their order: D / 4 lanes a row, four elements each.
+template <int D>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedParams p)
+{
+    typedef Part<D> P;
+    constexpr int LANES = D / 4, EACH = 256 / LANES;
+    const int per = p.groups0 + p.groups1, lane = threadIdx.x % LANES, parts = ROWS / EACH;
+    const int item = blockIdx.x / parts, in = (int)(blockIdx.x % parts) * EACH + threadIdx.x / LANES;
+    const int head = item / per, group = item - head * per, b = head / p.H, h = head - b * p.H;
+    const bool second = group >= p.groups0;
+    const int row = (second ? group - p.groups0 : group) * ROWS + in, length = second ? p.N - p.n0 : p.n0, t = min(row, length - 1) + (second ? p.n0 : 0);
+    const bool some = p.document[b * p.document_sb + t] >= 0;
+    const float* const part = p.partial + (long long)item * p.pieces * P::FLOATS;
+    float top = -1e30f;
+    for (int i = 0; i < p.pieces; ++i) top = fmaxf(top, part[i * P::FLOATS + P::REFERENCE + in]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int i = 0; i < p.pieces; ++i) {
+        const float* const from = part + i * P::FLOATS;
+        const float by = __builtin_amdgcn_exp2f(from[P::REFERENCE + in] - top);
+        acc += by * *(const f32x4*)(from + in * D + 4 * lane);
+        sum += by * from[P::SUM + in];
+    }
+    const float inverse = 1.f / sum;
+    float all = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) all = __builtin_fmaf(acc[r], 0.f, all);
+    // (rows that are not finite again, key by key, as above)
+    unsigned long long bad = __builtin_amdgcn_ballot_w64(all != 0.f && row < length && some);
+    const int first = threadIdx.x / 64 * (64 / LANES), own = threadIdx.x % 64 / LANES;
+    const unsigned long long mine = (LANES == 32 ? 0xffffffffull : 0xffffull) << (own * LANES);
+    if (row < length && (bad & mine) == 0ull) {
+        const Side& to = p.side[second];
+        bf16x4 out;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[r] = (__bf16)(some ? acc[r] * inverse : 0.f);
+        *(bf16x4*)(to.o + b * to.out_sb + h * to.out_sh + (long long)row * to.out_sn + 8 * lane) = out;
+    }
+    while (bad != 0ull) {
+        const int i = __builtin_ctzll(bad) / LANES;    // of the wavefront's rows
+        bad &= ~((LANES == 32 ? 0xffffffffull : 0xffffull) << (i * LANES));
+        const int row_again = (second ? group - p.groups0 : group) * ROWS + (int)(blockIdx.x % parts) * EACH + first + i;
+        row_by_keys<D>(p, b, h, row_again + (second ? p.n0 : 0), threadIdx.x % 64);
+    }
+}
+
+// Into how many pieces the tiles of every group are cut where the groups do not fill the card (a tile of a workgroup that has a CU to itself takes
+// 1.3 us, most of it waiting): as many as make 512 workgroups, of four tiles at least, or 768 of twelve.  us, whole / cut, one head of
+// 64 1000 tokens 26.9 / 16.2, 8000 172.8 / 43.4; five 4000 92.2 / 42.6, 8000 178.8 / 110.3; two of 128 1000 34.3 / 20.2, 4000 113.2 / 40.9 (into twelve
+// 48.5); eight of 128 2000 63.6 / 41.8 (768 workgroups of five tiles 47.5), 4000 116.0 / 76.0 (512 of 31 tiles 82.8).
+int pieces_for(long long groups, long long tiles)
+{
+    constexpr long long MOST = 8;
+    auto least = [](long long a, long long b) { return a < b ? a : b; };
+    const long long some = least(512 / groups, tiles / 4), more = least(768 / groups, tiles / 12), pieces = least(some > more ? some : more, MOST);
+    return pieces < 2 ? 1 : (int)pieces;
+}
+
+// The workspace: what is known of the tiles, the groups in order, the pieces
+struct Space {
+    size_t sorted, partial, bytes;
+};
+Space space_of(int B, int H, long long tiles, long long groups, int D, int pieces)
+{
+    Space s;
+    s.sorted = (size_t)B * tiles * sizeof(Known);
+    s.partial = s.sorted + ((size_t)B * groups * sizeof(int) + 15) / 16 * 16;
+    s.bytes = s.partial + (pieces > 1 ? (size_t)B * H * groups * pieces * sizeof(float) * (D == 64 ? Part<64>::FLOATS : Part<128>::FLOATS) : 0);
+    return s;
 }
 
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -707,8 +807,10 @@ extern "C" {
 size_t rapid_attn_packed_workspace_bytes(int B, int H, int N, int D)
 {
     if (B <= 0 || H <= 0 || N <= 0 || N > (1 << 22) || (long long)B * H > 524287 || (D != 64 && D != 128)) return 0;
-    const size_t tiles = (N + TILE - 1) / TILE + 1, groups = (N + ROWS - 1) / ROWS + 1;        // (one more where there are two segments)
-    return (size_t)B * (tiles * sizeof(Known) + (tiles <= PLANNED ? (groups + 3) / 4 * 16 : 0));
+    const long long tiles = (N + TILE - 1) / TILE + 1, groups = (N + ROWS - 1) / ROWS + 1;         // (one more where there are two segments)
+    const Space s = space_of(B, H, tiles, groups, D, pieces_for((long long)B * H * (groups - 1), tiles));
+    const Space whole = space_of(B, H, tiles, groups, D, 1);
+    return s.bytes > whole.bytes ? s.bytes : whole.bytes;
 }
 
 int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B, int H, int D, const int* document,
@@ -768,18 +870,26 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     p.groups0 = (p.n0 + ROWS - 1) / ROWS;
     p.groups1 = (n1 + ROWS - 1) / ROWS;
     const int per = p.groups0 + p.groups1, pairs = B * H;
+    p.pieces = pieces_for((long long)pairs * per, p.tiles);
+    const Space space = space_of(B, H, p.tiles, per, D, p.pieces);
+    p.partial = (float*)((char*)workspace + space.partial);
     p.known = p.tiles <= FEW ? nullptr : (Known*)workspace;
     if (!p.known) {
     } else if (p.tiles <= PLANNED) {
-        p.sorted = (int*)(p.known + (size_t)B * p.tiles);
+        p.sorted = (int*)((char*)workspace + space.sorted);
         hipLaunchKernelGGL(packed_plan_kernel, dim3((unsigned)B), dim3(1024), 0, (hipStream_t)stream, p);
     } else {
         hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 3) / 4), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
     }
-    const dim3 grid(8u * (unsigned)(pairs / 8 * per + (pairs % 8 * per + 7) / 8));
+    const dim3 grid(8u * (unsigned)(pairs / 8 * per + (pairs % 8 * per + 7) / 8) * (unsigned)p.pieces);
     auto kernel = D == 64 ? cap > 0.f ? packed_tiles_kernel<64, true> : packed_tiles_kernel<64, false>
                           : cap > 0.f ? packed_tiles_kernel<128, true> : packed_tiles_kernel<128, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(WAVES * 64), 0, (hipStream_t)stream, p);
+    if (p.pieces > 1) {
+        const int lanes = D / 4;
+        hipLaunchKernelGGL(D == 64 ? packed_join_kernel<64> : packed_join_kernel<128>, dim3((unsigned)(pairs * per) * (unsigned)(ROWS * lanes / 256)),
+                           dim3(256), 0, (hipStream_t)stream, p);
+    }
     return hipGetLastError() == hipSuccess ? RAPID_OK : RAPID_ERR_DEVICE;
 }
 
