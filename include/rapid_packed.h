@@ -96,9 +96,9 @@ RAPID_API size_t rapid_linear_int8_workspace_bytes(long long M, int N, int K);
  *   scale     as rapid_attn_dense
  *   workspace at least rapid_attn_packed_workspace_bytes(B, H, N, D) bytes, 16-byte aligned; contents on entry do not matter, nothing in it
  *             survives as state; one workspace must not serve two calls that can run concurrently
- *   constraints  D 64 or 128; q, k, v, o 16-byte aligned, strides multiples of 8 elements, in_stride_n and out_stride_n D .. 2^23, others
+ *   constraints  D 64 or 128; q, k, v, o 16-byte aligned, strides multiples of 8 elements, in_stride_n and out_stride_n D .. 2^23 - 8, others
  *             0 .. 2^40 (those of dimensions of size 1 not looked at); document, order 4-byte aligned, their strides 0 .. 2^40; N (of both
- *             segments) <= 2^22; B*H <= 524287; B*H*ceil(N/64) < 2^30
+ *             segments) <= 2^22; B*H <= 524287; B*H*(ceil(N/128) + 1) < 2^24 - 16
  * o shares no byte with an input.  Fastest where a document's tokens follow each other (within each segment).
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE; RAPID_ERR_UNSUPPORTED (D, cap, a scale that is not a number); RAPID_ERR_ALIGN; RAPID_ERR_WORKSPACE;
  * RAPID_ERR_ALIAS (o begins where a q, k, v or the other o does); RAPID_ERR_DEVICE.

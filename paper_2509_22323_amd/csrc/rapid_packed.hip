@@ -1,5 +1,6 @@
 // Attention of documents packed into one joint sequence, for MI355X (gfx950).  C ABI: include/rapid_packed.h.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 #include <stdint.h>
@@ -37,8 +38,9 @@ struct PackedParams {
     int* sorted;                                       // [B, groups], most work first, or null
     int pieces;                                        // of what a group has to do
     float* partial;                                    // [B, H, groups, pieces]: what a piece comes to
-    float scale;                                       // of a score: capped / log2(e), else as exponent of 2
+    float scale;                                       // of a score, as exponent of 2
     float cap;                                         // as exponent of 2; 0: none
+    float share;                                       // of the cap, of a score
     float small, series[5];                            // of a capped score: see series()
 };
 
@@ -55,15 +57,32 @@ __device__ __forceinline__ float sum_of_lanes(float v)
     return v;
 }
 
-// The exponent of 2 that a product q k stands for.
-__device__ __forceinline__ float exponent(float s, float scale, float cap)
+// tanh(u) / u as a polynomial in u^2, fitted to 1.0e-6 of it up to u = NEAR
+constexpr float NEAR = 0.8f;
+constexpr double TANH[5] = {0.999998994, -0.33325372, 0.132305656, -0.0491801422, 0.0121001386};
+
+// A value such that nothing made from it is kept in registers over a loop.
+template <class T>
+__device__ __forceinline__ T here(T v)
 {
-    if (cap == 0.f) return s * scale;
-    // cap tanh(u) = cap - 2 cap / (1 + exp(2 u)), scale = 2 log2(e) scale' / cap'
-    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * scale)), cap);
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
-// The same over s, where |s| <= p.small: tanh(u) / u as a polynomial in u^2, fitted to 1.0e-6 of it up to u = 0.8.
+// The exponent of 2 that a product s = q k stands for: s scale, or cap tanh(u), u = s share.
+__device__ __forceinline__ float exponent(float s, float scale, float cap, float share)
+{
+    if (cap == 0.f) return s * scale;
+    const float u = s * share, t = u * u;
+    // cap - 2 cap / (1 + exp(2 u)) is off by roundings of the cap: not where the cap is far above the score
+    const float far = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * (2.f * LOG2E))), cap);
+    float near = here((float)TANH[4]);
+#pragma unroll
+    for (int i = 3; i >= 0; --i) near = __builtin_fmaf(near, t, here((float)TANH[i]));
+    return fabsf(u) <= NEAR ? s * scale * near : far;
+}
+
+// The same over s where |s| <= p.small, the factors of all of it in the polynomial's.
 __device__ __forceinline__ float series(const PackedParams& p, float s)
 {
     const float t = s * s;
@@ -95,7 +114,7 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
 #pragma unroll
             for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)kv[i], (float)qv[i], s);
         }
-        s = exponent(s, p.scale, p.cap);
+        s = exponent(s, p.scale, p.cap, p.share);
         const float higher = fmaxf(m, most_of_lanes(seen ? s : -INFINITY));
         const float lower = m == higher ? 1.f : __builtin_amdgcn_exp2f(m - higher);
         m = higher;
@@ -357,11 +376,6 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
     const long long delta0 = p.side[0].v - p.side[0].k, delta1 = p.side[1].v - p.side[1].k;
     const int* const documents = p.document + b * p.document_sb;
     const int* const orders = p.order ? p.order + b * p.order_sb : nullptr;
-    // a value such that nothing made from it is kept in registers over the loop
-    auto here = [](auto v) {
-        asm volatile("" : "+v"(v));
-        return v;
-    };
     auto copy = [&](const Visit& e, auto is_v, auto slot) {
         constexpr bool V = is_v.value;
         const bool s = (e.high >> 30 & 1) != 0;
@@ -499,7 +513,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap);
+                        for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap, p.share);
                 size = cap;
             }
             look = __builtin_amdgcn_ballot_w64(size > fminf(m[0], m[1]) + 8.f) != 0ull;
@@ -798,6 +812,9 @@ Space space_of(int B, int H, long long tiles, long long groups, int D, int piece
     return s;
 }
 
+// (a launch has less than 2^32 lanes)
+inline bool too_large(int B, int H, long long N) { return (long long)B * H * ((N + ROWS - 1) / ROWS + 1) >= (1LL << 24) - 16; }
+
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 }  // namespace
@@ -806,7 +823,7 @@ extern "C" {
 
 size_t rapid_attn_packed_workspace_bytes(int B, int H, int N, int D)
 {
-    if (B <= 0 || H <= 0 || N <= 0 || N > (1 << 22) || (long long)B * H > 524287 || (D != 64 && D != 128)) return 0;
+    if (B <= 0 || H <= 0 || N <= 0 || N > (1 << 22) || (long long)B * H > 524287 || too_large(B, H, N) || (D != 64 && D != 128)) return 0;
     const long long tiles = (N + TILE - 1) / TILE + 1, groups = (N + ROWS - 1) / ROWS + 1;         // (one more where there are two segments)
     const Space s = space_of(B, H, tiles, groups, D, pieces_for((long long)B * H * (groups - 1), tiles));
     const Space whole = space_of(B, H, tiles, groups, D, 1);
@@ -831,13 +848,13 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
         long long in[3] = {B == 1 ? 0 : g.in_stride_b, H == 1 ? 0 : g.in_stride_h, g.n == 1 ? D : g.in_stride_n};
         long long out[3] = {B == 1 ? 0 : g.out_stride_b, H == 1 ? 0 : g.out_stride_h, g.n == 1 ? D : g.out_stride_n};
         for (long long* s : {in, out}) {
-            if (s[0] < 0 || s[0] > (1LL << 40) || s[1] < 0 || s[1] > (1LL << 40) || s[2] < D || s[2] > (1 << 23)) return RAPID_ERR_SHAPE;
+            if (s[0] < 0 || s[0] > (1LL << 40) || s[1] < 0 || s[1] > (1LL << 40) || s[2] < D || s[2] >= (1 << 23)) return RAPID_ERR_SHAPE;
             if ((s[0] | s[1] | s[2]) % 8 != 0) return RAPID_ERR_ALIGN;
         }
         if (!aligned(g.q, 16) || !aligned(g.k, 16) || !aligned(g.v, 16) || !aligned(g.o, 16)) return RAPID_ERR_ALIGN;
         p.side[i] = {(const char*)g.q, (const char*)g.k, (const char*)g.v, (char*)g.o, 2 * in[0], 2 * in[1], 2 * out[0], 2 * out[1], (int)(2 * in[2]), (int)(2 * out[2])};
     }
-    if (N > (1 << 22) || (long long)B * H * ((N + 63) / 64) >= (1LL << 30)) return RAPID_ERR_SHAPE;
+    if (N > (1 << 22) || too_large(B, H, N)) return RAPID_ERR_SHAPE;
     for (int i = 0; i < n_segments; ++i)
         for (int j = 0; j < n_segments; ++j) {
             const char* o = p.side[i].o;
@@ -855,13 +872,14 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     p.B = B;
     p.H = H;
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
-    p.cap = cap * LOG2E;
-    p.scale = cap > 0.f ? 2.f * LOG2E * scale / cap : scale * LOG2E;
-    // (the polynomial's factors are numbers of fp32 for all but caps that are out of proportion to the scale)
-    const double u = cap > 0.f ? (double)scale / cap : 0.0;
+    // (numbers of fp32, whatever cap and scale: a product of 0 has the exponent 0)
+    p.scale = fminf(scale * LOG2E, FLT_MAX);
+    p.cap = fminf(cap * LOG2E, FLT_MAX / 4);
+    p.share = cap > 0.f ? fminf(scale / cap, 0x1p96f) : 0.f;
+    // (as are the series' factors, for all but caps out of proportion to the scale)
+    const double u = p.share;
     if (u > 0x1p-12 && u < 0x1p12) {
-        constexpr double TANH[5] = {0.999998994, -0.33325372, 0.132305656, -0.0491801422, 0.0121001386};
-        p.small = (float)(0.8 / u);
+        p.small = (float)(NEAR / u);
         for (int i = 0; i < 5; ++i) p.series[i] = (float)(TANH[i] * p.cap * pow(u, 2 * i + 1));
     }
     const int n1 = p.N - p.n0;

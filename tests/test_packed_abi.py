@@ -114,7 +114,8 @@ def attend(segs=({},), B=1, H=2, D=64, document=9 * A, ds=4, order=None, os=4, c
     *((dict(segs=({name: None},)), NULL) for name in "qkvo"), *((dict(segs=({}, {**OTHER, name: None})), NULL) for name in "qkvo"),
     (dict(segs=({},) * 3), SHAPE), (dict(B=0), SHAPE), (dict(H=-1), SHAPE), (dict(B=1 << 10, H=1 << 10), SHAPE), (dict(segs=({"n": 0},)), SHAPE),
     (dict(segs=({"n": (1 << 22) + 1},)), SHAPE), (dict(segs=({"n": 1 << 22}, OTHER)), SHAPE), (dict(segs=({"in_n": 56},)), SHAPE),
-    (dict(segs=({"out_n": 0},)), SHAPE), (dict(segs=({"in_n": (1 << 23) + 8},)), SHAPE), (dict(segs=({"in_h": -64},)), SHAPE),
+    (dict(segs=({"out_n": 0},)), SHAPE), (dict(segs=({"in_n": (1 << 23) + 8},)), SHAPE), (dict(segs=({"in_n": 1 << 23},)), SHAPE), (dict(segs=({"out_n": 1 << 23},)), SHAPE),
+    (dict(B=1 << 8, H=1 << 8, segs=({"n": 1 << 15},)), SHAPE), (dict(segs=({"in_h": -64},)), SHAPE),
     (dict(segs=({"out_h": (1 << 40) + 8},)), SHAPE), (dict(B=2, segs=({"in_b": -8},)), SHAPE), (dict(B=2, ds=-1), SHAPE),
     (dict(B=2, order=A, os=-4), SHAPE), (dict(B=2, ds=(1 << 40) + 1), SHAPE), (dict(B=1 << 9, H=1 << 9, segs=({"n": 1 << 18},)), SHAPE),
     (dict(D=96), UNSUPPORTED), (dict(cap=-1.0), UNSUPPORTED), (dict(cap=float("inf")), UNSUPPORTED), (dict(cap=float("nan")), UNSUPPORTED),
@@ -135,7 +136,7 @@ def test_strides_of_dimensions_of_size_one_are_not_looked_at():
 
 
 @pytest.mark.parametrize("size", [(0, 1, 64, 64), (1, 0, 64, 64), (1, 1, 0, 64), (1, 1, (1 << 22) + 1, 64), (1, 1, 64, 96), (1 << 10, 1 << 10, 64, 64),
-                                  (1 << 32, 1, 64, 64), (1, 1, 1 << 32, 64)], ids=str)
+                                  (1 << 32, 1, 64, 64), (1, 1, 1 << 32, 64), (1 << 8, 1 << 8, 1 << 15, 64)], ids=str)
 def test_workspaces_of_sizes_that_are_refused(size):
     assert ra.rapid_attn_packed_workspace_bytes(*size) == 0
 
