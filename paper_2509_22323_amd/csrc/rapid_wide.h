@@ -42,6 +42,11 @@ __device__ __forceinline__ void sample_of(const P& p, int m, int& b, int& r)
     r = m - b * p.n;
 }
 
+// Products of whole numbers: the sum is exact, and behind it every rounding is written down here, so that no kernel's compiler joins a
+// multiplication and an addition that another's leaves apart: the same row gives the same bits in all of them.
+__device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale, float bias) { return __builtin_fmaf((float)sum * x_scale, w_scale, bias); }
+__device__ __forceinline__ float ended(float z, float gate, float residual) { return __builtin_fmaf(z, gate, residual); }
+
 // residual + gate * act(sum), everything in fp32, rounded once.  (What is not there is skipped by scalar branches.)
 template <class P>
 __device__ __forceinline__ bf16x8 finished(const P& p, float (&z)[8], bf16x8 gate, bf16x8 residual)
@@ -49,6 +54,12 @@ __device__ __forceinline__ bf16x8 finished(const P& p, float (&z)[8], bf16x8 gat
     if (p.activation != RAPID_ACT_NONE) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] = activated(z[i], p.activation);
+    }
+    if constexpr (std::is_same_v<P, Linear8Params>) {
+        bf16x8 out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = (__bf16)ended(z[i], p.gate ? (float)gate[i] : 1.f, p.residual ? (float)residual[i] : 0.f);
+        return out;
     }
     if (p.gate) {
 #pragma unroll
@@ -463,12 +474,8 @@ __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(P p, int items
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         auto both = __builtin_amdgcn_permlane16_swap(a[q], b[q], false, false);
-                        z[q] = (float)(int)both[0] * by * w_scale[c % HELD][0][q];
-                        z[4 + q] = (float)(int)both[1] * by * w_scale[c % HELD][1][q];
-                    }
-                    if (p.bias) {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) z[q] += (float)added[c % HELD][q];
+                        z[q] = scaled((int)both[0], by, w_scale[c % HELD][0][q], p.bias ? (float)added[c % HELD][q] : 0.f);
+                        z[4 + q] = scaled((int)both[1], by, w_scale[c % HELD][1][q], p.bias ? (float)added[c % HELD][4 + q] : 0.f);
                     }
                 } else {
 #pragma unroll

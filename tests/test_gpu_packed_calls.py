@@ -301,3 +301,32 @@ def test_many_samples_and_heads():
     want = v.clone()
     want[5] = 0
     assert same(got, want)
+
+
+@pytest.mark.parametrize("C", [2056, 2432, 2816, 4104, 4608, 6144, 8200, 9728, 12288, 12296])
+def test_norms_of_every_width(C):
+    from test_gpu_int8 import assert_normed
+    x = normal((1, 7, C), C, 2.0, 0.5)
+    s, t = normal((1, C), 1), normal((1, C), 2)
+    q, scale = torch.zeros((1, 7, C), dtype=torch.int8, device="cuda"), torch.zeros((1, 7), device="cuda")
+    ra.rapid_norm_modulate_int8(x, q, scale, s, t, 1e-6)
+    assert_normed(po.norm_modulate(widen(x), widen(s), widen(t), float(np.float32(1e-6))), (q, scale))
+
+
+@pytest.mark.parametrize("parts", [dict(), dict(bias=True), dict(gate=True), dict(residual=True), dict(bias=True, residual=True), dict(bias=True, gate=True, residual=True),
+                                   dict(gate=True, residual=True, document=True), dict(bias=True, act="silu", residual=True, document=True)], ids=str)
+@pytest.mark.parametrize("K,N,M", [(1552, 300, 2000), (144, 1000, 5000), (2432, 2432, 1100)], ids=str)
+def test_a_row_gives_the_same_bits_under_every_epilogue(parts, K, N, M):
+    x, w, xs, ws = codes((1, M, K), 1), codes((N, K), 2), scales((1, M), 3, 0.01), scales((N,), 4, 0.01)
+    d = torch.zeros((1, M), dtype=torch.int32, device="cuda") if parts.get("document") else None
+    b = normal((N,), 5) if parts.get("bias") else None
+    g = normal((1, N), 6) if parts.get("gate") else None
+    r = normal((1, M, N), 7, 30.0) if parts.get("residual") else None
+
+    def run(a, z):
+        return ra.rapid_linear_int8(x[:, a:z], xs[:, a:z].contiguous(), w, ws, torch.empty((1, z - a, N), dtype=torch.bfloat16, device="cuda"), b,
+                                    parts.get("act", "none"), g, None if r is None else r[:, a:z], None if d is None else d[:, a:z].contiguous())
+
+    whole = run(0, M)
+    for a, z in ((0, 1), (1, 3), (2, 6), (0, 8), (7, 24), (100, 164), (50, 400), (300, 1011)):
+        assert same(run(a, z), whole[:, a:z]), (a, z)
