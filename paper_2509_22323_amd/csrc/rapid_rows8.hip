@@ -347,6 +347,8 @@ int rapid_quantize_rows(const rapid_rows* x, const rapid_rows* q, float* scale, 
     RowsParams p = {};
     const int rc = rows_of(x, q, scale, B, n, K, 1 << 17, p);
     if (rc != RAPID_OK) return rc;
+    // As few wavefronts a row as hold it with four accesses a lane.  Memory is the bound, so that it matters little: us for 8192 rows of 1536 by
+    // 1 / 2 / 4 wavefronts 7.8 / 7.8 / 8.5, of 6144 by 2 / 4 / 8 29.5 / 28.4 / 27.8; any few hundred rows 3.7 to 4.4.
     if (K <= 512) return launch_quantize<1, 1>(p, stream);
     if (K <= 1024) return launch_quantize<1, 2>(p, stream);
     if (K <= 2048) return launch_quantize<1, 4>(p, stream);
@@ -379,12 +381,20 @@ int rapid_norm_modulate_int8(const rapid_rows* x, const rapid_rows* q, float* q_
     p.documents = documents;
     p.eps = eps;
     p.share = 1.0 / C;
-    if (C <= 512) return launch_norm<1, 1>(p, stream);
-    if (C <= 1024) return launch_norm<1, 2>(p, stream);
-    if (C <= 1536) return launch_norm<1, 3>(p, stream);
-    if (C <= 2048) return launch_norm<1, 4>(p, stream);
-    if (C <= 4096) return launch_norm<2, 4>(p, stream);
-    if (C <= 8192) return launch_norm<4, 4>(p, stream);
+    // As few wavefronts a row as hold it (joining sums of several costs three barriers a row), with no access that nothing is left for, and four
+    // wavefronts rather than two or eight of a longer one.  us, rows of 1536 by 1 / 2 / 4 wavefronts: 8192 of them 14.1 / 15.7 / 19.2; of 2432 by
+    // 1 x 6, 2 x 3, 4 x 2 accesses 21.1 / 21.7 / 25.8 (2 x 4: 23.9); of 6144 by 2 x 6, 4 x 3, 4 x 4, 8 x 2 51.4 / 47.5 / 52.5 / 55.6; 4096
+    // of 9728 by 4 x 6, 8 x 3, 8 x 4 42.7 / 47.6 / 51.7.  A few hundred rows take 5.3 to 6.3 us by any.
+    const int accesses = (C + 511) / 512;              // of a wavefront
+    if (accesses == 1) return launch_norm<1, 1>(p, stream);
+    if (accesses == 2) return launch_norm<1, 2>(p, stream);
+    if (accesses == 3) return launch_norm<1, 3>(p, stream);
+    if (accesses == 4) return launch_norm<1, 4>(p, stream);
+    if (accesses <= 6) return launch_norm<1, 6>(p, stream);
+    if (accesses <= 8) return launch_norm<2, 4>(p, stream);
+    if (accesses <= 12) return launch_norm<4, 3>(p, stream);
+    if (accesses <= 16) return launch_norm<4, 4>(p, stream);
+    if (accesses <= 24) return launch_norm<4, 6>(p, stream);
     return launch_norm<8, 4>(p, stream);
 }
 
