@@ -157,36 +157,59 @@ __device__ __forceinline__ int moved(int v)
 {
     return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
 }
-// f over the values of the wavefront, in every lane
+// f over the values of 8 and of 16 lanes, in each of them
 template <class F>
-__device__ __forceinline__ int over_lanes(int v, F f)
+__device__ __forceinline__ int over_8_lanes(int v, F f)
 {
     v = f(v, moved<0xB1>(v));                          // lane ^ 1
     v = f(v, moved<0x4E>(v));                          // lane ^ 2
-    v = f(v, moved<0x141>(v));                         // 7 - lane of every 8
-    v = f(v, moved<0x140>(v));                         // 15 - lane of every 16
-    auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    v = f((int)a[0], (int)a[1]);
-    auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return f((int)b[0], (int)b[1]);
+    return f(v, moved<0x141>(v));                      // 7 - lane of every 8
+}
+template <class F>
+__device__ __forceinline__ int over_16_lanes(int v, F f)
+{
+    v = over_8_lanes(v, f);
+    return f(v, moved<0x140>(v));                      // 15 - lane of every 16
 }
 
-// Of tile `tile` of a sample, by a wavefront.
+// Of tiles `tile` .. `tile` + 3 of a sample (the last one again behind it), by a wavefront: lanes 16 i .. 16 i + 15 know of tile + i.
+// (16 lanes a tile and four tokens a lane, not 64 lanes a tile: a quarter of the steps between lanes, which bind where a workgroup
+// does this alone.)
 __device__ __forceinline__ Known known_of(const PackedParams& p, int b, int tile, int lane)
 {
+    tile = min(tile + (lane >> 4), p.tiles - 1);
     const bool second = tile >= p.tiles0;
-    const int row = (second ? tile - p.tiles0 : tile) * TILE + lane, n = second ? p.N - p.n0 : p.n0;
-    const int t = min(row, n - 1) + (second ? p.n0 : 0);
-    const int d = p.document[b * p.document_sb + t], o = p.order ? p.order[b * p.order_sb + t] : 0;
-    const bool there = row < n && d >= 0;
+    const int row = (second ? tile - p.tiles0 : tile) * TILE + (lane & 15), n = second ? p.N - p.n0 : p.n0;
+    const int* const document = p.document + b * p.document_sb + (second ? p.n0 : 0);
+    const int* const order = p.order ? p.order + b * p.order_sb + (second ? p.n0 : 0) : nullptr;
+    int d[4], o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = min(row + 16 * i, n - 1);
+        d[i] = document[t];
+        o[i] = order ? order[t] : 0;
+    }
+    Known k = {INT_MAX, -1, order ? INT_MAX : 0, order ? INT_MIN : 0};
+    bool all = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool there = row + 16 * i < n && d[i] >= 0;
+        all = all && there;
+        if (!there) continue;
+        k.first = min(k.first, d[i]);
+        k.last = max(k.last, d[i]);
+        k.early = min(k.early, o[i]);
+        k.late = max(k.late, o[i]);
+    }
     auto least = [](int a, int b) { return min(a, b); };
     auto most = [](int a, int b) { return max(a, b); };
-    Known k = {over_lanes(there ? d : INT_MAX, least), over_lanes(there ? d : -1, most), 0, 0};
-    if (p.order) {
-        k.early = over_lanes(there ? o : INT_MAX, least);
-        k.late = over_lanes(there ? o : INT_MIN, most);
+    k.first = over_16_lanes(k.first, least);
+    k.last = over_16_lanes(k.last, most);
+    if (order) {
+        k.early = over_16_lanes(k.early, least);
+        k.late = over_16_lanes(k.late, most);
     }
-    if (__builtin_amdgcn_ballot_w64(!there) != 0ull) k.first = ~k.first;
+    if ((__builtin_amdgcn_ballot_w64(!all) >> (lane & 48) & 0xffffull) != 0ull) k.first = ~k.first;
     return k;
 }
 
@@ -223,39 +246,46 @@ constexpr int PLANNED = 1026;
 __global__ __launch_bounds__(1024) void packed_plan_kernel(PackedParams p)
 {
     __shared__ __align__(16) Known known[PLANNED];
-    __shared__ int visits[PLANNED / 2 + 1];
+    __shared__ __align__(16) int visits[(PLANNED / 2 + 1 + 3) / 4 * 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = p.groups0 + p.groups1, b = blockIdx.x;
-    for (int tile = wave; tile < p.tiles; tile += 16) {
-        const Known k = known_of(p, b, tile, lane);
-        if (lane == 0) {
+    for (int first = 4 * wave; first < p.tiles; first += 64) {
+        const Known k = known_of(p, b, first, lane);
+        const int tile = first + (lane >> 4);
+        if ((lane & 15) == 0 && tile < p.tiles) {
             known[tile] = k;
             p.known[(long long)b * p.tiles + tile] = k;
         }
     }
+    if (tid < 4) visits[per / 4 * 4 + tid] = -1;       // (read in fours)
     __syncthreads();
-    for (int group = wave; group < per; group += 16) {
+    for (int first = 0; first < per; first += 128) {   // eight lanes a group
+        const int group = min(first + tid / 8, per - 1);
         const Known mine = known_of_group(p, known, group);
         int count = 0;
-        for (int t = 0; t < p.tiles; t += 64)
-            count += __popcll(__builtin_amdgcn_ballot_w64(t + lane < p.tiles && sees(mine, known[min(t + lane, p.tiles - 1)]) != NONE));
-        if (lane == 0) visits[group] = count;
+        for (int tile = tid % 8; tile < p.tiles; tile += 8) count += sees(mine, known[tile]) != NONE;
+        count = over_8_lanes(count, [](int a, int b) { return a + b; });
+        if (tid % 8 == 0) visits[group] = count;       // (the last one by several, all of which have counted the same)
     }
     __syncthreads();
     for (int group = tid; group < per; group += 1024) {
         int before = 0;
         const int own = visits[group];
-        for (int i = 0; i < per; ++i) before += visits[i] > own || (visits[i] == own && i < group);
+#pragma unroll 4
+        for (int i = 0; i < per; i += 4) {
+            const i32x4 others = *(const i32x4*)(visits + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) before += others[j] > own || (others[j] == own && i + j < group);
+        }
         p.sorted[(long long)b * per + before] = group;
     }
 }
 
-// What is known of all tiles, a wavefront each.
+// What is known of all tiles, four a wavefront.
 __global__ __launch_bounds__(256) void packed_known_kernel(PackedParams p)
 {
-    const int lane = threadIdx.x & 63, tile = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (tile >= p.tiles) return;
-    const Known k = known_of(p, blockIdx.y, tile, lane);
-    if (lane == 0) p.known[(long long)blockIdx.y * p.tiles + tile] = k;
+    const int lane = threadIdx.x & 63, first = 4 * (blockIdx.x * 4 + (threadIdx.x >> 6)), tile = first + (lane >> 4);
+    const Known k = known_of(p, blockIdx.y, first, lane);
+    if ((lane & 15) == 0 && tile < p.tiles) p.known[(long long)blockIdx.y * p.tiles + tile] = k;
 }
 
 // ---------------------------------------------------------------------------
@@ -342,10 +372,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
     const int length = second ? p.N - p.n0 : p.n0, row0 = (second ? group - p.groups0 : group) * ROWS;
     const Known* const known = p.known + (long long)b * p.tiles;
     if (!p.known) {                                    // few tiles: every workgroup looks at them itself, which is faster than a launch before it
-        for (int tile = wave; tile < p.tiles; tile += WAVES) {
-            const Known k = known_of(p, b, tile, lane);
-            if (lane == 0) own_known[tile] = k;
-        }
+        static_assert(FEW == 4 * WAVES, "");
+        const Known k = known_of(p, b, 4 * wave, lane);
+        if (lane % 16 == 0) own_known[4 * wave + lane / 16] = k;
         __syncthreads();
     }
     const Known mine = p.known ? known_of_group(p, known, group) : known_of_group(p, own_known, group);
@@ -897,7 +926,7 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
         p.sorted = (int*)((char*)workspace + space.sorted);
         hipLaunchKernelGGL(packed_plan_kernel, dim3((unsigned)B), dim3(1024), 0, (hipStream_t)stream, p);
     } else {
-        hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 3) / 4), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL(packed_known_kernel, dim3((unsigned)((p.tiles + 15) / 16), (unsigned)B), dim3(256), 0, (hipStream_t)stream, p);
     }
     const dim3 grid(8u * (unsigned)(pairs / 8 * per + (pairs % 8 * per + 7) / 8) * (unsigned)p.pieces);
     auto kernel = D == 64 ? cap > 0.f ? packed_tiles_kernel<64, true> : packed_tiles_kernel<64, false>

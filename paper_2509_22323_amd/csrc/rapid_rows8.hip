@@ -212,7 +212,7 @@ __device__ __forceinline__ double larger_of(double a, double b)
 // The norm, in fp64: what it ends in are whole numbers, and a result in 32 bits would be on another side of a border between two of them than
 // the formula's about once in 10^5 elements, at another place for every order of the sums.  (The card adds and multiplies as fast
 // in 64 bits as in 32.)
-template <int WAVES, int CHUNKS>
+template <int WAVES, int CHUNKS, bool FULL>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kernel(RowsParams p)
 {
     constexpr int BLOCK = WAVES < 4 ? 256 : WAVES * 64, ROWS = BLOCK / 64 / WAVES, LANES = WAVES * 64;
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
     for (int c = 0; c < CHUNKS; ++c) {
         const int at = 8 * (c * LANES + lane);
         const u32x4 none = {0u, 0u, 0u, 0u};
-        raw[c] = at < p.C ? *(const u32x4*)(x + at) : none;
+        raw[c] = FULL || at < p.C ? *(const u32x4*)(x + at) : none;
     }
     const int d = p.document ? p.document[m] : b;
     const bool written = there && (!p.document || (unsigned)d < (unsigned)p.documents);
@@ -248,10 +248,10 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
     double y[CHUNKS][8], square = 0.0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const bool in = 8 * (c * LANES + lane) < p.C;
+        const double off = FULL || 8 * (c * LANES + lane) < p.C ? mean : 0.0;         // (beyond the row: zeros)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            y[c][i] = in ? (double)(i % 2 ? high(raw[c][i / 2]) : low(raw[c][i / 2])) - mean : 0.0;
+            y[c][i] = (double)(i % 2 ? high(raw[c][i / 2]) : low(raw[c][i / 2])) - off;
             square = __builtin_fma(y[c][i], y[c][i], square);
         }
     }
@@ -260,23 +260,21 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int at = 8 * (c * LANES + lane);
-        if (at >= p.C) continue;
+        if (!FULL && at >= p.C) continue;
         if (p.scale && written) {
             const u32x4 scale = *(const u32x4*)(p.scale + d * p.scale_s + at), shift = *(const u32x4*)(p.shift + d * p.shift_s + at);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const double by = 1.0 + (double)(i % 2 ? high(scale[i / 2]) : low(scale[i / 2]));
                 y[c][i] = __builtin_fma(y[c][i] * inv, by, (double)(i % 2 ? high(shift[i / 2]) : low(shift[i / 2])));
+                number = __builtin_fma(y[c][i], 0.0, number);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[c][i] *= inv;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            most = larger(most, y[c][i]);
-            if (p.scale) number = __builtin_fma(y[c][i], 0.0, number);
-        }
+        for (int i = 0; i < 8; ++i) most = larger(most, y[c][i]);
     }
     most = larger(most, number != 0.0 ? INFINITY : 0.0);
     most = over_waves<WAVES>(over_lanes(most, larger), part[2], wave, own, larger);
@@ -287,7 +285,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kerne
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int at = 8 * (c * LANES + lane);
-        if (at >= p.C) continue;
+        if (!FULL && at >= p.C) continue;
         unsigned w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = (unsigned)__double2loint(__builtin_fma(y[c][i], by, 6755399441055744.0));   // 1.5 * 2^52
@@ -312,7 +310,8 @@ template <int WAVES, int CHUNKS>
 int launch_norm(const RowsParams& p, void* stream)
 {
     constexpr int BLOCK = WAVES < 4 ? 256 : WAVES * 64, ROWS = BLOCK / 64 / WAVES;
-    hipLaunchKernelGGL((norm_rows8_kernel<WAVES, CHUNKS>), dim3((unsigned)((p.M + ROWS - 1) / ROWS)), dim3(BLOCK), 0, (hipStream_t)stream, p);
+    const auto kernel = p.C == WAVES * CHUNKS * 512 ? norm_rows8_kernel<WAVES, CHUNKS, true> : norm_rows8_kernel<WAVES, CHUNKS, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((p.M + ROWS - 1) / ROWS)), dim3(BLOCK), 0, (hipStream_t)stream, p);
     return launched();
 }
 
