@@ -71,7 +71,7 @@ __device__ __forceinline__ int sum_of_lanes(int v)
 }
 
 // A handful of rows (the conditioning's projections): a wavefront takes OUT outputs of all rows and reads their rows of w end to end, 1 KB an
-// access, four products an instruction.  Bound by the bytes of w.
+// access, four products an instruction.  Bound by the bytes of w and the launch: 2 rows, 1536 to 9216, 4.9 us (14 MB: 2.9 TB/s).
 constexpr int OUT = 2, DOT_WAVES = 2;
 
 template <int MAX_M>

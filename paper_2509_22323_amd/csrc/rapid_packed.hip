@@ -238,10 +238,14 @@ __device__ __forceinline__ Known known_of_group(const PackedParams& p, const Kno
     return mine;
 }
 
-constexpr int FEW = 16;                                // tiles that every workgroup looks at itself
+// Tiles that every workgroup looks at itself, before its queries have come; a launch before it takes 3 us: 2 heads of 64, 256 tokens 9.5 us (12.6
+// with the launch), 24 of 128, 512 23.8 (26.8), 1024 37.0 (40.1).  More would be a second round of loads in every workgroup.
+constexpr int FEW = 16;
 
 // What is known of all tiles, and the groups of a sample in the order of what they have to do, most first: workgroups go to the CUs in
-// turn as these get free, so that what is left for last is short.  A workgroup a sample, of PLANNED tiles at most.
+// turn as these get free, so that what is left for last is short.  24 heads of 128, documents of 4608, 1101, 1357 and 376 tokens: 298 us, in the
+// order of the sequence 314; where documents are alike it costs up to 3 %: 8200 tokens one by one 407 and 400 us.  Beyond PLANNED
+// tiles, which LDS would not hold beside their groups, there are groups enough, and the last ones go first.  A workgroup a sample: 8 us.
 constexpr int PLANNED = 1026;
 __global__ __launch_bounds__(1024) void packed_plan_kernel(PackedParams p)
 {
@@ -290,7 +294,19 @@ __global__ __launch_bounds__(256) void packed_known_kernel(PackedParams p)
 
 // ---------------------------------------------------------------------------
 // The kernel: a workgroup takes 128 queries of a head, a wavefront 32 of them, and goes over the tiles that one of them sees.
-// S^T = K Q^T, one query a lane, and O^T += V^T P^T, v_mfma_f32_16x16x32_bf16; P goes from one product to the next in registers.
+// S^T = K Q^T, one query a lane, and O^T += V^T P^T, v_mfma_f32_16x16x32_bf16; P goes from one product to the next in registers, and
+// o = sum p v / sum p with p = 2^(x - m), x the exponents and m a reference that only moves when one is 2^8 above it, so that
+// accumulators are rescaled a few times a row.  p is rounded to bf16 for the product, and the sum is of the rounded values.
+// Tiles that every query sees whole take no mask at all; others compare the documents and orders that were copied beside their values.
+//
+// Two tiles of keys and two of values in LDS, copied past the registers a whole step ahead, one barrier a step; in a step the scores of the
+// next tile and the sums of this one are matrix instructions, between which the vector work on the weights is dealt out by hand.
+// Bound at D = 128 by the matrix pipe and the clock under it: 32 heads of 4096 tokens in 254 to 264 us (1.08 to 1.04 PFLOP/s), pipe and vector
+// units busy half of the cycles each; without the barriers 2 % less time, without exponents 2.5 %.  At D = 64 by the vector instructions, which are the
+// same for half the products: 161 to 165 us (0.84 PFLOP/s).  A cap is seven instructions a score more, where its polynomial serves: 322 to 334 us at
+// D = 128, 234 at D = 64 (vector units 87 % busy).  Workgroups a CU: two of 230 registers at D = 128, three of 168 at 64.
+// 256 queries a workgroup at D = 128: 5 % less time for one document, 5 to 18 % more for documents of a few hundred tokens.  64 queries a
+// wavefront at D = 64 (half the reads of LDS): 10 % more, with two wavefronts a SIMD for three.
 // ---------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) char lds_char;
 
@@ -464,7 +480,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         }
     };
     auto mask = [&](const Visit& e, auto slot, f32x4 (&s)[4][2]) {
-        const int lane_ = here(lane), n = lane_ & 15, g = lane_ >> 4;
+        const int own_lane = here(lane), n = own_lane & 15, g = own_lane >> 4;
         lds_char* const at = (lds_char*)lds + 4 * L::BYTES + 2 * slot.value * 4 * TILE + 16 * g;
         const int doc[2] = {mine_doc[32 * wave + n], mine_doc[32 * wave + 16 + n]}, turn[2] = {mine_turn[32 * wave + n], mine_turn[32 * wave + 16 + n]};
 #pragma unroll
@@ -513,10 +529,16 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         return v;
     };
     float most[2];                                     // of this lane's scores of a tile
+    constexpr std::integral_constant<int, 0> zero;
+    constexpr std::integral_constant<int, 1> one;
+    constexpr std::integral_constant<int, 2> two;
+    constexpr std::integral_constant<int, 3> three;
+    constexpr std::true_type values;
+    constexpr std::false_type keys;
     // The weights of a tile whose scores are s, and what they add, beside the scores of the next one.  Items: one operand from LDS, requested
     // AHEAD items before, and the matrix instructions of both groups of queries; behind each a quarter or two of the work on a pair of weights.
-    auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], auto turn_) {
-        constexpr int T = turn_.value;                 // K of this tile in slot T, V in slot 2 + T
+    auto step = [&](const Visit& e, f32x4 (&s)[4][2], f32x4 (&next)[4][2], auto slot) {
+        constexpr int T = slot.value;                  // K of this tile in slot T, V in slot 2 + T
         // (a bound on a capped tile's scores is at hand with the choice of its formula, so their maximum is looked for only where that is too large)
         bool look = true;
         if constexpr (CAP) {                           // (before the mask: what is hidden is not -cap)
@@ -548,7 +570,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
             look = __builtin_amdgcn_ballot_w64(size > fminf(m[0], m[1]) + 8.f) != 0ull;
         }
         if ((int)e.high < 0) {
-            mask(e, turn_, s);
+            mask(e, slot, s);
             partly = true;
         }
         if ((int)e.high < 0 || (CAP && look)) {
@@ -606,13 +628,12 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
                 sums[q] = __builtin_amdgcn_fdot2_f32_bf16(both, ones, sums[q], false);
             }
         };
-        constexpr std::integral_constant<int, 0> begin;
-        each(begin, std::integral_constant<int, AHEAD>(), request);
-        each(begin, std::integral_constant<int, ALL>(), [&](auto item) {
+        each(zero, std::integral_constant<int, AHEAD>(), request);
+        each(zero, std::integral_constant<int, ALL>(), [&](auto item) {
             constexpr int I = item.value, half = I < QK + PV ? 0 : 1;
             if constexpr (I + AHEAD < ALL) request(std::integral_constant<int, I + AHEAD>());
-            each(begin, std::integral_constant<int, 2>(), [&](auto query) {
-                constexpr int q = query.value, at = 2 * I + q;     // 2 I + q: matrix instructions before this one
+            each(zero, two, [&](auto query) {
+                constexpr int q = query.value, at = 2 * I + q;     // matrix instructions before this one
                 if constexpr (I < QK) {
                     constexpr int kt = I % 4, k = I / 4;
                     const f32x4 none = {0.f, 0.f, 0.f, 0.f};
@@ -669,13 +690,6 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
             return Visit{(unsigned)__builtin_amdgcn_readfirstlane(e.low), (unsigned)__builtin_amdgcn_readfirstlane(e.high),
                          __builtin_amdgcn_readfirstlane(e.bytes), __builtin_amdgcn_readfirstlane(e.token)};
         };
-        constexpr std::integral_constant<int, 0> zero;
-        constexpr std::integral_constant<int, 1> one;
-        constexpr std::integral_constant<int, 2> two;
-        constexpr std::integral_constant<int, 3> three;
-        constexpr std::true_type values;
-        constexpr std::false_type keys;
-
         // K: slots 0 and 1, V: slots 2 and 3
         f32x4 even[4][2], odd[4][2];
         Visit now = visit(0), then = count > 1 ? visit(1) : now;
@@ -712,7 +726,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         arrive();                                      // before the list and the slots serve the next tiles
     }
 
-    const int lane_here = here(lane), n_here = lane_here & 15, g_here = lane_here >> 4;
+    const int end_lane = here(lane), end_n = end_lane & 15, end_g = end_lane >> 4;       // (not kept over the loop)
     float sum[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -724,10 +738,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         float* const part = p.partial + (((long long)head * per + group) * p.pieces + piece) * P::FLOATS;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const int row = 32 * wave + 16 * q + n_here;
+            const int row = 32 * wave + 16 * q + end_n;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) *(f32x4*)(part + row * D + 16 * d + 4 * g_here) = acc[d][q];
-            if (g_here == 0) {
+            for (int d = 0; d < DT; ++d) *(f32x4*)(part + row * D + 16 * d + 4 * end_g) = acc[d][q];
+            if (end_g == 0) {
                 part[P::SUM + row] = sum[q];
                 part[P::REFERENCE + row] = m[q];
             }
@@ -739,8 +753,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
     unsigned again = 0;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const int row = q0 + 16 * q + n_here;
-        const bool some = mine_doc[32 * wave + 16 * q + n_here] >= 0;
+        const int row = q0 + 16 * q + end_n;
+        const bool some = mine_doc[32 * wave + 16 * q + end_n] >= 0;
         const float inverse = 1.f / sum[q];
         float all = 0.f;
 #pragma unroll
@@ -750,8 +764,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         const unsigned long long bad = partly ? __builtin_amdgcn_ballot_w64(all != 0.f && row < length && some) : 0ull;
         const unsigned rows = (unsigned)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu;
         again |= rows << (16 * q);
-        if (row >= length || (rows >> n_here & 1) != 0) continue;
-        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * g_here;
+        if (row >= length || (rows >> end_n & 1) != 0) continue;
+        char* o = own.o + b * own.out_sb + h * own.out_sh + (long long)row * own.out_sn + 8 * end_g;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             bf16x4 out;
@@ -766,7 +780,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         asm volatile("" : "+s"(sample));
         const int i = __builtin_ctz(again);
         again &= again - 1;
-        row_by_keys<D>(p, sample, h, q0 + i + (second ? p.n0 : 0), lane_here);
+        row_by_keys<D>(p, sample, h, q0 + i + (second ? p.n0 : 0), end_lane);
     }
 }
 
