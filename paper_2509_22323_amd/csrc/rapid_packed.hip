@@ -69,24 +69,32 @@ __device__ __forceinline__ T here(T v)
     return v;
 }
 
-// The exponent of 2 that a product s = q k stands for: s scale, or cap tanh(u), u = s share.
-__device__ __forceinline__ float exponent(float s, float scale, float cap, float share)
+// The exponent of 2 that a product s = q k stands for: s scale, or cap tanh(u), u = s share.  Of two formulas of the latter, by |u| alone, so that a
+// result does not depend on what else a tile holds: the polynomial, or cap - 2 cap / (1 + exp(2 u)), which is off by roundings of the cap.
+__device__ __forceinline__ float beyond(float s, float cap, float share)
 {
-    if (cap == 0.f) return s * scale;
-    const float u = s * share, t = u * u;
-    // cap - 2 cap / (1 + exp(2 u)) is off by roundings of the cap: not where the cap is far above the score
-    const float far = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * (2.f * LOG2E))), cap);
-    float near = here((float)TANH[4]);
-#pragma unroll
-    for (int i = 3; i >= 0; --i) near = __builtin_fmaf(near, t, here((float)TANH[i]));
-    return fabsf(u) <= NEAR ? s * scale * near : far;
+    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * share * (2.f * LOG2E))), cap);
 }
-
-// The same over s where |s| <= p.small, the factors of all of it in the polynomial's.
+// |s| <= p.small, the factors of all of it in the polynomial's
 __device__ __forceinline__ float series(const PackedParams& p, float s)
 {
     const float t = s * s;
     return __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(p.series[4], t, p.series[3]), t, p.series[2]), t, p.series[1]), t, p.series[0]);
+}
+// any s, where p.small is 0: those factors would not be numbers of fp32
+__device__ __forceinline__ float out_of_proportion(float s, float scale, float cap, float share)
+{
+    const float u = s * share, t = u * u;
+    float near = here((float)TANH[4]);
+#pragma unroll
+    for (int i = 3; i >= 0; --i) near = __builtin_fmaf(near, t, here((float)TANH[i]));
+    return fabsf(u) <= NEAR ? s * scale * near : beyond(s, cap, share);
+}
+__device__ __forceinline__ float exponent(const PackedParams& p, float s)
+{
+    if (p.cap == 0.f) return s * p.scale;
+    if (p.small == 0.f) return out_of_proportion(s, p.scale, p.cap, p.share);
+    return fabsf(s) <= p.small ? s * series(p, s) : beyond(s, p.cap, p.share);
 }
 
 // One row of the output by one wavefront, key by key: a lane a key for the scores, D / 64 elements of the output a lane.
@@ -114,7 +122,7 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
 #pragma unroll
             for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)kv[i], (float)qv[i], s);
         }
-        s = exponent(s, p.scale, p.cap, p.share);
+        s = exponent(p, s);
         const float higher = fmaxf(m, most_of_lanes(seen ? s : -INFINITY));
         const float lower = m == higher ? 1.f : __builtin_amdgcn_exp2f(m - higher);
         m = higher;
@@ -461,6 +469,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
     bool partly = false;
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
     typedef __attribute__((address_space(3))) const i32x4 lds_i32x4;
+    typedef __attribute__((address_space(3))) i32x4 lds_i32x4_out;
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const float scale = p.scale, cap = p.cap;
@@ -486,6 +495,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
             const i32x4 d = *(lds_i32x4*)(at + 64 * kt);
+            // Values of no document: zeros, before this wavefront reads them (others write the same), so that what padding holds costs nothing.
+            if (__builtin_amdgcn_ballot_w64(min(min(d[0], d[1]), min(d[2], d[3])) < 0) != 0ull) {
+                const int row = here(own_lane), none = here(0);
+                lds_char* const to = (lds_char*)lds + (2 + slot.value) * L::BYTES + (16 * kt + 4 * (row >> 4)) * L::RB + 16 * (row & 15);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (d[r] < 0 && (row & 15) < D / 8) *(lds_i32x4_out*)(to + r * L::RB) = i32x4{none, none, none, none};
+            }
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -549,8 +566,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
                 for (int q = 0; q < 2; ++q)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) size = fmaxf(size, fabsf(s[kt][q][r]));
-            const bool small = __builtin_amdgcn_ballot_w64(size > p.small) == 0ull;
-            if (__builtin_expect(small, 1)) {
+            const bool all_small = __builtin_amdgcn_ballot_w64(size > p.small) == 0ull;
+            if (__builtin_expect(all_small, 1)) {
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
@@ -558,13 +575,24 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[kt][q][r] *= series(p, s[kt][q][r]);
                 size *= series(p, size);
+            } else if (p.small != 0.f) {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float x = s[kt][q][r];
+                            s[kt][q][r] = fabsf(x) <= p.small ? x * series(p, x) : beyond(x, cap, p.share);
+                        }
+                size = cap;
             } else {
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[kt][q][r] = exponent(s[kt][q][r], scale, cap, p.share);
+                        for (int r = 0; r < 4; ++r) s[kt][q][r] = out_of_proportion(s[kt][q][r], scale, cap, p.share);
                 size = cap;
             }
             look = __builtin_amdgcn_ballot_w64(size > fminf(m[0], m[1]) + 8.f) != 0ull;
@@ -697,6 +725,12 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         copy(now, values, two);
         if (count > 1) copy(then, keys, one);
         arrive();
+        // (zeros for queries of no document: what they hold is not to move the references of others)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            if (mine_doc[32 * wave + 16 * q + (here(lane) & 15)] < 0)
+#pragma unroll
+                for (int k = 0; k < KS; ++k) qf[q][k] = bf16x8{};
         scores(zero, even);
 #pragma unroll
         for (int q = 0; q < 2; ++q) most[q] = largest(even, q);

@@ -330,3 +330,27 @@ def test_a_row_gives_the_same_bits_under_every_epilogue(parts, K, N, M):
     whole = run(0, M)
     for a, z in ((0, 1), (1, 3), (2, 6), (0, 8), (7, 24), (100, 164), (50, 400), (300, 1011)):
         assert same(run(a, z), whole[:, a:z]), (a, z)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
+@pytest.mark.parametrize("n,m,H", [(300, 0, 2), (1300, 0, 1), (200, 90, 2), (700, 700, 24)], ids=str)
+def test_what_padding_holds_changes_no_bit(D, cap, n, m, H):
+    """Tokens of no document between the others and behind them, in tiles that others share"""
+    N = n + m
+    d = documents(N, (N // 2, N // 3), seed=5 if H == 2 else None)
+    q, k, v = normal((3, 1, H, N, D), 6)
+    dt = torch.from_numpy(d).cuda()
+
+    def run():
+        o = torch.full((1, H, N, D), 7.0, dtype=torch.bfloat16, device="cuda")
+        ra.rapid_attn_packed([tuple(t[:, :, a:z] for t in (q, k, v, o)) for a, z in ((0, n), (n, N)) if z > a], dt, cap=cap)
+        return o
+
+    for t in (q, k, v):
+        t[:, :, d < 0] = 0
+    want = run()
+    for value in (NAN, float("inf"), -1.5e38):
+        for t in (q, k, v):
+            t[:, :, d < 0] = value
+        assert same(run(), want), value
