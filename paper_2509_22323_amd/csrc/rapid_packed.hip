@@ -108,11 +108,11 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
     const char* q = at.q + b * at.in_sb + h * at.in_sh + (long long)row * at.in_sn;
     const int own = document[t], turn = order ? order[t] : 0;
     constexpr int EACH = D / 64;
-    float acc[EACH] = {}, m = -INFINITY, l = 0.f;
+    float acc[EACH] = {}, m = -1e30f, l = 0.f;       // (m finite, so that a score of -infinity is a weight of 0)
     for (int first = 0; own >= 0 && first < p.N; first += 64) {
         const int j = min(first + lane, p.N - 1);
         const bool seen = first + lane < p.N && document[j] == own && (!order || order[j] <= turn);
-        unsigned long long keys = __builtin_amdgcn_ballot_w64(seen);
+        const unsigned long long keys = __builtin_amdgcn_ballot_w64(seen);
         if (keys == 0ull) continue;
         const Side& from = p.side[j >= p.n0];
         const char* k = from.k + b * from.in_sb + h * from.in_sh + (long long)(j >= p.n0 ? j - p.n0 : j) * from.in_sn;
@@ -130,15 +130,25 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
         l = l * lower + sum_of_lanes(e);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) acc[i] *= lower;
-        while (keys != 0ull) {
-            const int i = __builtin_ctzll(keys), key = first + i;
-            keys &= keys - 1ull;
-            const Side& from = p.side[key >= p.n0];
-            const char* v = from.v + b * from.in_sb + h * from.in_sh + (long long)(key >= p.n0 ? key - p.n0 : key) * from.in_sn;
-            const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e), i));
-            const __bf16* of = (const __bf16*)v + EACH * lane;
+        if (l != l) break;                             // (so are all of the row's results)
+        constexpr int AT_ONCE = 8;                     // whose values are on their way together
+        for (int i = 0; i < 64; i += AT_ONCE) {
+            if ((keys >> i & 0xffull) == 0ull) continue;
+            float value[AT_ONCE][EACH];
 #pragma unroll
-            for (int c = 0; c < EACH; ++c) acc[c] = __builtin_fmaf(by, (float)of[c], acc[c]);
+            for (int c = 0; c < AT_ONCE; ++c) {
+                const int key = min(first + i + c, p.N - 1);
+                const Side& from = p.side[key >= p.n0];
+                const __bf16* v = (const __bf16*)(from.v + b * from.in_sb + h * from.in_sh + (long long)(key >= p.n0 ? key - p.n0 : key) * from.in_sn) + EACH * lane;
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) value[c][j] = (float)v[j];
+            }
+#pragma unroll
+            for (int c = 0; c < AT_ONCE; ++c) {
+                const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e), i + c));
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) acc[j] = __builtin_fmaf(by, (keys >> (i + c) & 1ull) != 0ull ? value[c][j] : 0.f, acc[j]);
+            }
         }
     }
     __bf16* o = (__bf16*)(at.o + b * at.out_sb + h * at.out_sh + (long long)row * at.out_sn) + EACH * lane;
