@@ -15,6 +15,11 @@
 
 namespace {
 
+constexpr int STEP = 64;                               // inputs per step
+constexpr int CUS = 256;
+constexpr int MOST_PIECES = 8;                         // along K
+static_assert(STEP == INPUTS<__bf16>, "");
+
 // The sums of a product's pieces, in their order, and the epilogue: eight outputs a lane.
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p)
 {
@@ -185,7 +190,7 @@ constexpr TileCost COST[TILES] = {
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
     const long long items = ((M + c.rows - 1) / c.rows) * ((N + c.columns - 1) / c.columns) * pieces, slots = CUS * c.slots;
-    const int all = (K + STEP<__bf16> - 1) / STEP<__bf16>;
+    const int all = (K + STEP - 1) / STEP;
     const float steps = all > 2 ? (float)all / pieces : 2.f, load = (float)(items % slots) / CUS;
     const float ends = N % 8 != 0 && pieces == 1 ? c.ends + c.odd : c.ends;
     float t = c.call + (float)(items / slots) * (steps * c.full + ends);
@@ -203,7 +208,7 @@ Plan plan_for(long long M, int N, int K, int most_pieces)
     for (int t = 0; t < TILES; ++t) {
         // (a piece has three steps at least; larger tiles have work enough, or few steps; a lane number of the join has 32 bits)
         const int most = t <= T128x128 && M * N < (1LL << 31) ? most_pieces : 1;
-        for (int pieces = 1; pieces <= most && (pieces == 1 || 3 * pieces * STEP<__bf16> <= K); ++pieces) {
+        for (int pieces = 1; pieces <= most && (pieces == 1 || 3 * pieces * STEP <= K); ++pieces) {
             const float c = cost_of(COST[t], M, N, K, pieces);
             if (c < least) { least = c; best = {(Tile)t, pieces}; }
         }

@@ -11,6 +11,11 @@
 
 namespace {
 
+constexpr int STEP = 128;                              // inputs per step
+constexpr int CUS = 256;
+constexpr int MOST_PIECES = 8;                         // along K
+static_assert(STEP == INPUTS<signed char>, "");
+
 // The row of the gate that row m takes (sample b); below 0: the row is not written.
 __device__ __forceinline__ int vector_of(const Linear8Params& p, int m, int b)
 {
@@ -188,12 +193,11 @@ constexpr TileCost COST[TILES] = {
     {64, 64, 4, 0.324f, 1.047f, 1.30f, 2.06f, 3.42f, 2.32f, 1.90f}, {128, 128, 2, 0.502f, 1.091f, 3.28f, 3.19f, 2.31f, 1.87f, 1.93f},
     {256, 128, 1, 0.481f, 1.020f, 4.05f, 3.23f, 3.03f, 0.f, 0.f},   {256, 160, 1, 0.669f, 1.308f, 5.56f, 3.43f, 2.90f, 0.f, 0.f},
     {256, 192, 1, 0.654f, 1.299f, 6.30f, 4.78f, 2.19f, 0.f, 0.f},   {256, 256, 1, 0.820f, 1.645f, 8.02f, 5.66f, 2.57f, 0.f, 0.f}};
-constexpr int INPUTS = STEP<signed char>;              // of a step
 
 float cost_of(const TileCost& c, long long M, int N, int K, int pieces)
 {
     const long long items = ((M + c.rows - 1) / c.rows) * ((N + c.columns - 1) / c.columns) * pieces, slots = CUS * c.slots;
-    const int all = (K + INPUTS - 1) / INPUTS;
+    const int all = (K + STEP - 1) / STEP;
     const float steps = all > 2 ? (float)all / pieces : 2.f, load = (float)(items % slots) / CUS;
     const float ends = N % 8 != 0 && pieces == 1 ? c.ends + c.odd : c.ends;
     float t = c.call + (float)(items / slots) * (steps * c.full + ends);
@@ -211,7 +215,7 @@ Plan plan_for(long long M, int N, int K, int most_pieces)
     for (int t = 0; t < TILES; ++t) {
         // (a piece has three steps at least; larger tiles have work enough, or few steps; a lane number of the join has 32 bits)
         const int most = t <= T128x128 && M * N < (1LL << 31) ? most_pieces : 1;
-        for (int pieces = 1; pieces <= most && (pieces == 1 || 3 * pieces * INPUTS <= K); ++pieces) {
+        for (int pieces = 1; pieces <= most && (pieces == 1 || 3 * pieces * STEP <= K); ++pieces) {
             const float c = cost_of(COST[t], M, N, K, pieces);
             if (c < least) { least = c; best = {(Tile)t, pieces}; }
         }

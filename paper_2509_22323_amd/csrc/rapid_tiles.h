@@ -132,7 +132,6 @@ __device__ __forceinline__ void store_eight(__bf16* at, int j, int N, bf16x8 v, 
     }
 }
 
-constexpr int CUS = 256;
 constexpr unsigned NOWHERE = 0xC0000000u;              // an offset outside any buffer below
 constexpr unsigned BUFFER = 0x81000000u;               // bytes that a tile's rows may span, and the inputs of a row
 

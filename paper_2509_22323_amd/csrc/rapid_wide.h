@@ -94,15 +94,14 @@ __device__ __forceinline__ bf16x8 finished(const P& p, float (&z)[8], bf16x8 gat
 // ---------------------------------------------------------------------------
 constexpr int ROW = 128;                               // bytes of a row per step
 template <class T>
-constexpr int STEP = ROW / (int)sizeof(T);             // inputs per step
-constexpr int MOST_PIECES = 8;                         // along K
+constexpr int INPUTS = ROW / (int)sizeof(T);           // of a step
 
 template <int WR, int FN, bool SPLIT, class P>
 __global__ __launch_bounds__(WR * 128, 2) void linear_wide_kernel(P p, int items)
 {
     typedef typename P::Type T;
     constexpr bool WHOLES = std::is_same_v<T, signed char>;           // products of whole numbers: sums in 32 bits, scales behind them
-    constexpr int SIZE = sizeof(T), STEP = ::STEP<T>;
+    constexpr int SIZE = sizeof(T), STEP = INPUTS<T>;
     typedef std::conditional_t<WHOLES, i32x4, bf16x8> Operand;
     typedef std::conditional_t<WHOLES, i32x4, f32x4> Sum;
     constexpr int FM = 4, TM = 64 * WR, TN = 32 * FN, WAVES = 2 * WR, PER_CU = 4 / WR;
