@@ -319,10 +319,10 @@ __global__ __launch_bounds__(256) void packed_known_kernel(PackedParams p)
 //
 // Two tiles of keys and two of values in LDS, copied past the registers a whole step ahead, one barrier a step; in a step the scores of the
 // next tile and the sums of this one are matrix instructions, between which the vector work on the weights is dealt out by hand.
-// Bound at D = 128 by the matrix pipe and the clock under it: 32 heads of 4096 tokens in 254 to 264 us (1.08 to 1.04 PFLOP/s), pipe and vector
+// Bound at D = 128 by the matrix pipe and the clock under it: 32 heads of 4096 tokens in 254 to 269 us from card to card (1.08 to 1.02 PFLOP/s), pipe and vector
 // units busy half of the cycles each; without the barriers 2 % less time, without exponents 2.5 %.  At D = 64 by the vector instructions, which are the
-// same for half the products: 161 to 165 us (0.84 PFLOP/s).  A cap is seven instructions a score more, where its polynomial serves: 322 to 334 us at
-// D = 128, 234 at D = 64 (vector units 87 % busy).  Workgroups a CU: two of 230 registers at D = 128, three of 168 at 64.
+// same for half the products: 161 to 170 us (0.85 to 0.81 PFLOP/s).  A cap is seven instructions a score more, where its polynomial serves: 322 to 341 us at
+// D = 128, 234 to 240 at D = 64 (vector units 87 % busy).  Workgroups a CU: two of 230 registers at D = 128, three of 168 at 64.
 // 256 queries a workgroup at D = 128: 5 % less time for one document, 5 to 18 % more for documents of a few hundred tokens.  64 queries a
 // wavefront at D = 64 (half the reads of LDS): 10 % more, with two wavefronts a SIMD for three.
 // ---------------------------------------------------------------------------

@@ -73,7 +73,7 @@ def test_products_have_the_workgroups_that_they_count_on(compiled, WR, FN, split
 def test_the_attention_loop_keeps_scalars_in_scalar_registers(compiled, D, cap):
     loop = one(compiled[1], f"packed_tiles_kernelILi{D}ELb{cap}E")
     assert sum(i.startswith("v_mfma") for i in loop) % (D // 2) == 0           # a tile or two
-    assert not [i for i in loop if i.startswith(("v_writelane", "scratch"))] and len([i for i in loop if i.startswith("v_readlane")]) <= 16
+    assert not [i for i in loop if i.startswith(("v_writelane", "scratch"))] and len([i for i in loop if i.startswith("v_readlane")]) <= 20
 
 
 @pytest.mark.parametrize("WR,FN,split", WIDE)
