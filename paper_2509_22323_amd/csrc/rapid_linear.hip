@@ -127,6 +127,7 @@ __global__ __launch_bounds__(DOT_WAVES * 64) void linear_dot_kernel(LinearParams
 
 // Every wavefront reads all of x.  Five to eight rows, three sets of inputs in turn: 10.6 to 11.0 us here, 11.5 in tiles of matrix
 // instructions at 1536 -> 9216, 8.9 to 9.2 and 11.5 at 6144 -> 1536, but 21 and 16.7 at 2432 -> 14592.  (Four: 7.7, 6.9 and 14.2 here.)
+// Up to four always: include/rapid_layer.h says that the bits of their rows do not depend on how many there are.
 bool by_dots(long long M, int N, int K) { return M <= 4 || (M <= 8 && (long long)N * K <= 1 << 24); }
 
 // Rows of y, residual and gate that start at multiples of four bytes, or results too small for it to matter: 8192 rows, 1536 -> 4607 with

@@ -119,14 +119,17 @@ class JointLayer:
 class PackedLayer:
     """The same layer in 8 bits over packed requests: the image tokens of all of them one after the other in one tensor, their texts in
     another, each request (a document) under a conditioning vector of its own and seeing itself alone.  The projections are products of
-    8-bit integers with scales for each token and channel; what a token comes to does not depend on what it is packed with, but for
-    the order in which its attention's sums are added.
+    8-bit integers with scales for each token and channel, and those of the conditioning, in bf16, are made of up to four requests at a
+    time, whose sums are each request's own; what a token comes to does not depend on what it is packed with, but for the order in
+    which its attention's sums are added.
 
     weights as JointLayer takes them; those of the projections are quantised here and not kept.  image, text: tokens that the
     tensors of a run have, any numbers; documents: how many requests a run holds at most; axes (RopeAxis each): the rotation of
     queries and keys, None = none.  F is a multiple of 16."""
 
     PRODUCTS = ("qkv_w", "out_w", "ff_in_w", "ff_out_w")
+    # Rows of a product in bf16 that are each by itself (of more, sums are added in another order for other numbers of them)
+    ROWS = 4
 
     def __init__(self, weights, H, D, image, text, documents, axes=None, layout="interleaved", eps=1e-6):
         import torch
@@ -156,9 +159,8 @@ class PackedLayer:
         self.f = [empty(n, F) for n, F in zip(self.tokens, wide)]
         self.f8 = [rows(n, F) for n, F in zip(self.tokens, wide)]
         self.table = None if axes is None else empty(image + text, sum(int(a.dim) for a in axes) // 2, 2, dtype=torch.float32)
-        need = max(max(_b.rapid_linear_int8_workspace_bytes(M, N, K) for n, F in zip(self.tokens, wide)
-                       for M, N, K in ((n, 3 * C, C), (n, C, C), (n, F, C), (n, C, F))),
-                   max(_b.rapid_linear_workspace_bytes(m, 6 * C, C) for m in range(1, documents + 1)))
+        need = max(_b.rapid_linear_int8_workspace_bytes(M, N, K) for n, F in zip(self.tokens, wide)
+                   for M, N, K in ((n, 3 * C, C), (n, C, C), (n, F, C), (n, C, F)))
         self.workspace = empty(max(need, 16), dtype=torch.uint8)
         self.attention_workspace = empty(max(_b.rapid_attn_packed_workspace_bytes(1, H, image + text, D), 16), dtype=torch.uint8)
         self.rows = [tuple(t.permute(2, 0, 3, 1, 4)) for t in self.qkv]            # (q, k, v) [1, H, n, D] of each stream
@@ -189,6 +191,7 @@ class PackedLayer:
         n = self.tokens[0]
         documents = (document[:n], document[n:])
         mods = [mod[:conditioning.shape[0]] for mod in self.mod]
+        requests = conditioning.split(self.ROWS)
         if positions is not None:
             _b.rapid_rope_table(positions, self.axes, self.table)
 
@@ -196,7 +199,8 @@ class PackedLayer:
             _b.rapid_linear_int8(*of, *w[name], out, bias, *rest, document=document, workspace=self.workspace)
 
         for x, h, mod, qkv, w, small, d in zip(hidden, self.h, mods, self.qkv, self.weights, self.small, documents):
-            _b.rapid_linear(conditioning, small["mod_w"], mod.view(mod.shape[0], -1), small["mod_b"], workspace=self.workspace)
+            for some, out in zip(requests, mod.view(mod.shape[0], -1).split(self.ROWS)):
+                _b.rapid_linear(some, small["mod_w"], out, small["mod_b"])
             _b.rapid_norm_modulate_int8(x, *h, mod[:, 1], mod[:, 0], self.eps, d)
             linear(h, w, "qkv_w", small["qkv_b"], qkv.view(x.shape[0], -1))
         _b.rapid_qk_norm_rope([(q, k, q, k) for q, k, _ in self.rows], self.norms, self.table, self.layout, self.eps)
