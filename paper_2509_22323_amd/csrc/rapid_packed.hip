@@ -108,7 +108,7 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
     const char* q = at.q + b * at.in_sb + h * at.in_sh + (long long)row * at.in_sn;
     const int own = document[t], turn = order ? order[t] : 0;
     constexpr int EACH = D / 64;
-    float acc[EACH] = {}, m = -1e30f, l = 0.f;       // (m finite, so that a score of -infinity is a weight of 0)
+    float acc[EACH] = {}, m = -INFINITY, l = 0.f;
     for (int first = 0; own >= 0 && first < p.N; first += 64) {
         const int j = min(first + lane, p.N - 1);
         const bool seen = first + lane < p.N && document[j] == own && (!order || order[j] <= turn);
@@ -126,7 +126,8 @@ __device__ void row_by_keys(const PackedParams& p, int b, int h, int t, int lane
         const float higher = fmaxf(m, most_of_lanes(seen ? s : -INFINITY));
         const float lower = m == higher ? 1.f : __builtin_amdgcn_exp2f(m - higher);
         m = higher;
-        const float e = seen ? __builtin_amdgcn_exp2f(s - m) : 0.f;
+        // (a score of -infinity is a weight of 0, also where there is no other yet)
+        const float e = seen ? __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.f : m)) : 0.f;
         l = l * lower + sum_of_lanes(e);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) acc[i] *= lower;
@@ -793,7 +794,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         return;
     }
 
-    // Results.  A weight of 0 times an infinity or NaN in a tile that not every query sees whole is NaN: such rows again, key by key.
+    // Results.  A weight of 0 times an infinity or NaN in a tile that not every query sees whole is NaN: such rows again, key by key.  So
+    // are rows without a weight: no exponent of theirs is above the -1e30 that the references begin with.
     unsigned again = 0;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -805,7 +807,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void packed_tiles_kern
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 4; ++r) all = __builtin_fmaf(acc[d][q][r], 0.f, all);
-        const unsigned long long bad = partly ? __builtin_amdgcn_ballot_w64(all != 0.f && row < length && some) : 0ull;
+        const unsigned long long bad = __builtin_amdgcn_ballot_w64((sum[q] == 0.f || (partly && all != 0.f)) && row < length && some);
         const unsigned rows = (unsigned)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu;
         again |= rows << (16 * q);
         if (row >= length || (rows >> end_n & 1) != 0) continue;
@@ -855,8 +857,8 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedParams p)
     float all = 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) all = __builtin_fmaf(acc[r], 0.f, all);
-    // (rows that are not finite again, key by key, as above)
-    unsigned long long bad = __builtin_amdgcn_ballot_w64(all != 0.f && row < length && some);
+    // (rows that are not finite or have no weight again, key by key, as above)
+    unsigned long long bad = __builtin_amdgcn_ballot_w64((all != 0.f || sum == 0.f) && row < length && some);
     const int first = threadIdx.x / 64 * (64 / LANES), own = threadIdx.x % 64 / LANES;
     const unsigned long long mine = (LANES == 32 ? 0xffffffffull : 0xffffull) << (own * LANES);
     if (row < length && (bad & mine) == 0ull) {

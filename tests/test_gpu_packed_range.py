@@ -1,0 +1,61 @@
+"""rapid_attn_packed at the ends of its range: scores, caps, scales and values far from 1."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2509_22323_amd as ra
+from layer_common import BF16_STEP, NAN, assert_within, normal, widen
+from oracle import packed_oracle as po
+from test_gpu_attn_packed import bound, documents
+from test_gpu_packed_calls import attend, form  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N,H", [(200, 2), (1500, 1), (1500, 40)], ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("cap,scale,size", [(0.0, 0.0, 1e16), (1e32, 0.0, 1e16), (1e32, 1e30, 10.0)], ids=str)
+def test_rows_whose_scores_are_all_far_below_zero(D, N, H, causal, cap, scale, size):
+    """Scores of -10^32 and less, and no others, in some documents (a single token, three of equal scores, two of which one's is twice the
+    other's) beside ordinary ones; in few tiles, in tiles that several workgroups share, and where a group has a workgroup to itself.
+    Equal scores are equal weights, and the least of two such scores has none."""
+    lengths = (70, 1, 3, 2, N - 100)
+    d, at = documents(N, lengths), np.cumsum((0,) + lengths)
+    order = np.arange(N, dtype=np.int32) if causal else None
+    q, k, v = normal((3, 1, H, N, D), 3)
+    if scale:                                          # (ordinary scores under it)
+        q[:, :, :at[1]] *= scale ** -0.5 / 4
+        k[:, :, :at[1]] *= scale ** -0.5 / 4
+        q[:, :, at[4]:] *= scale ** -0.5 / 4
+        k[:, :, at[4]:] *= scale ** -0.5 / 4
+    q[:, :, at[1]:at[4]], k[:, :, at[1]:at[4]] = size, -size
+    k[:, :, at[3] + 1] = -2 * size
+    got = widen(attend(q, k, v, torch.from_numpy(d).cuda(), None if order is None else torch.from_numpy(order).cuda(), cap, scale))
+    values = widen(v)
+    assert np.isfinite(got).all() and not got[:, :, at[5]:].any()
+    assert np.array_equal(got[:, :, at[1]], values[:, :, at[1]])
+    for i in range(3):
+        seen = values[:, :, at[2]:at[2] + (i + 1 if causal else 3)]
+        assert (np.abs(got[:, :, at[2] + i] - seen.mean(2)) <= BF16_STEP * np.abs(seen.mean(2)) + 2.0 ** -21 * np.abs(seen).mean(2)).all()
+    if not cap:
+        assert np.array_equal(got[:, :, at[3]:at[4]], np.broadcast_to(values[:, :, at[3]:at[3] + 1], got[:, :, at[3]:at[4]].shape))
+    if H < 40:
+        s = scale if scale else D ** -0.5
+        for a, z in ((0, at[1]), (at[4], at[5])):
+            part = [widen(t)[:, :, a:z] for t in (q, k, v)]
+            turn = None if order is None else order[None, a:z]
+            o, p = po.attention(*part, d[None, a:z], turn, cap, s)
+            # (a cap far above the scores costs them nothing but in proportion)
+            assert (np.abs(got[:, :, a:z] - o) <= bound(*part, p, o, 0.0, s, po.visible(d[None, a:z], turn))).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N", [1, 64, 150, 1280])
+def test_whole_tiles_far_below_zero(D, N):
+    """One document, every score -8e32 or less: tiles that need no mask"""
+    q, k, v = normal((3, 1, 1, N, D), 4)
+    q[:], k[:] = 1e16, -1e16
+    got = widen(attend(q, k, v, torch.zeros(N, dtype=torch.int32, device="cuda")))
+    mean, size = widen(v).mean(2, keepdims=True), np.abs(widen(v)).mean(2, keepdims=True)
+    assert (np.abs(got - mean) <= BF16_STEP * np.abs(mean) + (N + 2) * 2.0 ** -23 * size).all()
