@@ -965,11 +965,14 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     p.scale = fminf(scale * LOG2E, FLT_MAX);
     p.cap = fminf(cap * LOG2E, FLT_MAX / 4);
     p.share = cap > 0.f ? fminf(scale / cap, 0x1p96f) : 0.f;
-    // (as are the series' factors, for all but caps out of proportion to the scale)
+    // The series' factors, cap u^(2 i + 1), are numbers of fp32 for all but caps and scales out of proportion to each other or to 1.
     const double u = p.share;
     if (u > 0x1p-12 && u < 0x1p12) {
         p.small = (float)(NEAR / u);
-        for (int i = 0; i < 5; ++i) p.series[i] = (float)(TANH[i] * p.cap * pow(u, 2 * i + 1));
+        for (int i = 0; i < 5; ++i) {
+            p.series[i] = (float)(TANH[i] * p.cap * pow(u, 2 * i + 1));
+            if (isinf(p.series[i])) p.small = 0.f;
+        }
     }
     const int n1 = p.N - p.n0;
     p.tiles0 = (p.n0 + TILE - 1) / TILE;

@@ -59,3 +59,23 @@ def test_whole_tiles_far_below_zero(D, N):
     got = widen(attend(q, k, v, torch.zeros(N, dtype=torch.int32, device="cuda")))
     mean, size = widen(v).mean(2, keepdims=True), np.abs(widen(v)).mean(2, keepdims=True)
     assert (np.abs(got - mean) <= BF16_STEP * np.abs(mean) + (N + 2) * 2.0 ** -23 * size).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap,scale", [(1e14, 1e17), (1e5, 1e9), (1e30, 1e32)], ids=str)
+def test_caps_under_which_a_power_series_leaves_fp32(D, cap, scale):
+    """Ordinary scores (products of q and k are as small as the scale is large) far below the cap, which takes nothing away"""
+    q, k, v = normal((3, 1, 2, 150, D), 4)
+    q, k = q * (scale ** -0.5 / 4), k * (scale ** -0.5 / 4)
+    d = np.stack([documents(150, (100, 50))])
+    got = attend(q, k, v, torch.from_numpy(d).cuda(), cap=cap, scale=scale)
+    o, p = po.attention(widen(q), widen(k), widen(v), d, None, cap, scale)
+    assert_within(got, o, bound(widen(q), widen(k), widen(v), p, o, 0.0, scale, po.visible(d)))
+
+
+@pytest.mark.parametrize("cap,scale", [(1e14, 1e17), (1e35, 3e38), (1e5, 1e9), (1e30, 1e32), (1e-20, 1e-17)], ids=str)
+def test_products_of_zero_under_any_cap(cap, scale):
+    q, k, v = normal((3, 1, 2, 100, 64), 4)
+    got = attend(q * 0, k, v, torch.zeros(100, dtype=torch.int32, device="cuda"), cap=cap, scale=scale)
+    want, size = (np.broadcast_to(t.mean(2, keepdims=True), t.shape) for t in (widen(v), np.abs(widen(v))))
+    assert_within(got, want, BF16_STEP * np.abs(want) + 102 * 2.0 ** -23 * size)
