@@ -964,7 +964,7 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     // (numbers of fp32, whatever cap and scale: a product of 0 has the exponent 0)
     p.scale = fminf(scale * LOG2E, FLT_MAX);
     p.cap = fminf(cap * LOG2E, FLT_MAX / 4);
-    p.share = cap > 0.f ? fminf(scale / cap, 0x1p96f) : 0.f;
+    p.share = cap > 0.f ? fminf(scale / cap, FLT_MAX) : 0.f;
     // The series' factors, cap u^(2 i + 1), are numbers of fp32 for all but caps and scales out of proportion to each other or to 1.
     const double u = p.share;
     if (u > 0x1p-12 && u < 0x1p12) {

@@ -79,3 +79,16 @@ def test_products_of_zero_under_any_cap(cap, scale):
     got = attend(q * 0, k, v, torch.zeros(100, dtype=torch.int32, device="cuda"), cap=cap, scale=scale)
     want, size = (np.broadcast_to(t.mean(2, keepdims=True), t.shape) for t in (widen(v), np.abs(widen(v))))
     assert_within(got, want, BF16_STEP * np.abs(want) + 102 * 2.0 ** -23 * size)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("to,cap", [(2.0 ** 110, 0.5), (2.0 ** 119, 2.0 ** -20), (2.0 ** 100, 1.0)], ids=str)
+def test_scales_far_above_the_cap(D, to, cap):
+    """Products of q and k of 2^-98 or so under a scale that takes them beyond the cap: every score is the cap or its negative"""
+    q, k, v = normal((3, 1, 2, 150, D), 4)
+    k = (torch.where(k[..., :1] > 0, 1.0, -1.0) * 2.0 ** -52).expand_as(k).contiguous().to(k.dtype)
+    q = torch.ones_like(q) * 2.0 ** -52
+    d = np.stack([documents(150, (100, 50))])
+    got = attend(q, k, v, torch.from_numpy(d).cuda(), cap=cap, scale=to)
+    o, p = po.attention(widen(q), widen(k), widen(v), d, None, cap, to)
+    assert_within(got, o, bound(0 * widen(q), widen(k), widen(v), p, o, cap, to, po.visible(d)))
