@@ -92,8 +92,8 @@ RAPID_API size_t rapid_linear_int8_workspace_bytes(long long M, int N, int K);
  *             the segments' strides need not be the same
  *   document  device, int32, that of token t of sample b at document + b*document_stride_b + t (t over the joint sequence)
  *   order     device, int32, at order + b*order_stride_b + t, or NULL
- *   cap       0: none; else > 0 and finite
- *   scale     as rapid_attn_dense
+ *   cap       0: none; else > 0 and finite; one above 5.896e37 counts as that
+ *   scale     as rapid_attn_dense; one above 2.358e38 counts as that
  *   workspace at least rapid_attn_packed_workspace_bytes(B, H, N, D) bytes, 16-byte aligned; contents on entry do not matter, nothing in it
  *             survives as state; one workspace must not serve two calls that can run concurrently
  *   constraints  D 64 or 128; q, k, v, o 16-byte aligned, strides multiples of 8 elements, in_stride_n and out_stride_n D .. 2^23 - 8, others

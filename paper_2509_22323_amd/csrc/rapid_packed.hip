@@ -961,9 +961,11 @@ int rapid_attn_packed(const rapid_attn_segment* segments, int n_segments, int B,
     p.B = B;
     p.H = H;
     if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
-    // (numbers of fp32, whatever cap and scale: a product of 0 has the exponent 0)
+    // (numbers of fp32, whatever cap and scale: a product of 0 has the exponent 0; a cap that is cut is cut for its share of a score, too)
+    scale = fminf(scale, FLT_MAX / LOG2E);
+    cap = fminf(cap, FLT_MAX / 4 / LOG2E);
     p.scale = fminf(scale * LOG2E, FLT_MAX);
-    p.cap = fminf(cap * LOG2E, FLT_MAX / 4);
+    p.cap = cap * LOG2E;
     p.share = cap > 0.f ? fminf(scale / cap, FLT_MAX) : 0.f;
     // The series' factors, cap u^(2 i + 1), are numbers of fp32 for all but caps and scales out of proportion to each other or to 1.
     const double u = p.share;

@@ -92,3 +92,17 @@ def test_scales_far_above_the_cap(D, to, cap):
     got = attend(q, k, v, torch.from_numpy(d).cuda(), cap=cap, scale=to)
     o, p = po.attention(widen(q), widen(k), widen(v), d, None, cap, to)
     assert_within(got, o, bound(0 * widen(q), widen(k), widen(v), p, o, cap, to, po.visible(d)))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap,scale", [(3e38, 1e35), (1e38, 1e35), (5e37, 1e35), (3e38, 0.0)], ids=str)
+def test_caps_near_the_largest_number(D, cap, scale):
+    """Ordinary scores stay what they are under them"""
+    q, k, v = normal((3, 1, 2, 150, D), 4)
+    s = scale if scale else D ** -0.5
+    if scale:
+        q, k = q * (scale ** -0.5 / 4), k * (scale ** -0.5 / 4)
+    d = np.stack([documents(150, (100, 50))])
+    got = attend(q, k, v, torch.from_numpy(d).cuda(), cap=cap, scale=scale)
+    o, p = po.attention(widen(q), widen(k), widen(v), d, None, cap, s)
+    assert_within(got, o, bound(widen(q), widen(k), widen(v), p, o, 0.0, s, po.visible(d)))
