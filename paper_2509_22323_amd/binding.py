@@ -1001,8 +1001,8 @@ def rapid_attn_packed(segments, document, order=None, cap=0.0, scale=0.0, worksp
     """Attention of documents packed into one joint sequence: token i takes part in token j's softmax where document[i] == document[j]
     >= 0 and order[i] <= order[j] (order None: wherever the documents agree); tokens of no document (-1) output zeros.  `segments`:
     one or two (q, k, v, o) as rapid_attn_joint takes them, of any lengths; document, order: CUDA int32 [B,N] or [N] over the joint
-    tokens; cap > 0: scores s become cap * tanh(s / cap).  `workspace`: CUDA uint8 tensor of at least
-    rapid_attn_packed_workspace_bytes(B, H, N, D) bytes; allocated with torch if None.
+    tokens; cap > 0: scores s become cap * tanh(s / cap).  Caps and scales are numbers of fp32: what that holds as 0 is refused.
+    `workspace`: CUDA uint8 tensor of at least rapid_attn_packed_workspace_bytes(B, H, N, D) bytes; allocated with torch if None.
     Inference only: not recorded by autograd, no gradients.  Returns the o tensors."""
     if workspace is not None:                     # (the native form allocates nothing)
         status = (_native or _load_native()).packed_attention(segments, document, order, cap, scale, workspace)
@@ -1010,6 +1010,9 @@ def rapid_attn_packed(segments, document, order=None, cap=0.0, scale=0.0, worksp
             _check_packed(status)
             return [seg[3] for seg in segments]
     import torch
+    for name, value in (("cap", cap), ("scale", scale)):
+        if value > 0 and ctypes.c_float(value).value == 0:
+            raise ValueError(f"{name}: {value} is 0 in fp32, which would stand for " + ("no cap" if name == "cap" else "1/sqrt(D)"))
     descr, B, H, N, D = _segments(segments)
     q0 = segments[0][0]
     device = q0.get_device()

@@ -624,6 +624,8 @@ PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     long long document_stride, order_stride = 0;
     float cap, scale;
     if (n != 6 || !joint_segments(a[0], x) || !current(x.device) || !number(a[3], cap) || !number(a[4], scale)) Py_RETURN_NONE;
+    for (int i = 3; i < 5; ++i)                        // (more than 0, and 0 in fp32)
+        if (double d; number(a[i], d) && d > 0.0 && (float)d == 0.f) Py_RETURN_NONE;
     for (int i = 0; i < x.n; ++i)                      // (segments of different devices)
         if (THPVariable_Unpack(PySequence_Fast_GET_ITEM(PySequence_Fast_GET_ITEM(a[0], i), 0)).get_device() != x.device) Py_RETURN_NONE;
     if (!per_token(a[1], x, document, document_stride) || (a[2] != Py_None && !per_token(a[2], x, order, order_stride))) Py_RETURN_NONE;

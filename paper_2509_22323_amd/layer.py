@@ -178,8 +178,8 @@ class PackedLayer:
         for name, t in (("document", document), ("order", order)):
             if t is not None and tuple(t.shape) != (sum(self.tokens),):
                 raise ValueError(f"{name} must be [{sum(self.tokens)}], not {list(t.shape)}")
-        if not 0 <= cap < float("inf"):
-            raise ValueError("cap must be finite and not negative")
+        if not (cap == 0 or 2.0 ** -149 <= cap < 2.0 ** 128):
+            raise ValueError("cap must be 0 or a positive number of fp32")
         import torch
         if torch._C._cuda_getDevice() == self.device:
             return self._run(image, text, conditioning, document, positions, order, cap)

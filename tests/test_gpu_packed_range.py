@@ -106,3 +106,13 @@ def test_caps_near_the_largest_number(D, cap, scale):
     got = attend(q, k, v, torch.from_numpy(d).cuda(), cap=cap, scale=scale)
     o, p = po.attention(widen(q), widen(k), widen(v), d, None, cap, s)
     assert_within(got, o, bound(widen(q), widen(k), widen(v), p, o, 0.0, s, po.visible(d)))
+
+
+@pytest.mark.parametrize("kw", [dict(cap=1e-46), dict(cap=1e-300), dict(scale=1e-46), dict(cap=2.0, scale=5e-324)], ids=str)
+def test_caps_and_scales_that_fp32_holds_as_zero(form, kw):  # noqa: F811
+    """They would be taken for no cap and for the usual scale"""
+    q, k, v = normal((3, 1, 2, 100, 64), 4)
+    o = torch.full_like(q, 7.0)
+    with pytest.raises(ValueError):
+        attend(q, k, v, torch.zeros(100, dtype=torch.int32, device="cuda"), o=o, **kw)
+    assert (o == 7.0).all()

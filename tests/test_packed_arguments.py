@@ -1,0 +1,26 @@
+"""Host-only checks of arguments that fp32 does not hold as they are; no GPU needed."""
+import pytest
+import torch
+
+import paper_2509_22323_amd as ra
+from paper_2509_22323_amd import layer as layer_module
+from test_packed_layer import make, no_calls  # noqa: F401
+
+
+@pytest.mark.parametrize("kw", [dict(cap=1e-46), dict(scale=1e-46), dict(cap=5e-324, scale=1.0)], ids=str)
+def test_caps_and_scales_that_fp32_holds_as_zero(kw):
+    """0 would be no cap, or the usual scale: refused before the tensors are looked at"""
+    q = torch.zeros((1, 2, 4, 64), dtype=torch.bfloat16)
+    for workspace in (None, torch.zeros(4096, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            ra.rapid_attn_packed([(q, q, q, q)], torch.zeros(4, dtype=torch.int32), workspace=workspace, **kw)
+    with pytest.raises(TypeError):
+        ra.rapid_attn_packed([(q, q, q, q)], torch.zeros(4, dtype=torch.int32), cap=1e-44, scale=1e-44)
+
+
+@pytest.mark.parametrize("cap", [1e-46, 4e38])
+def test_caps_of_a_layer(cap, monkeypatch):
+    layer = make()
+    monkeypatch.setattr(layer_module, "_b", None)
+    with pytest.raises(ValueError):
+        layer.run(torch.zeros(77, 128), torch.zeros(9, 128), torch.zeros(3, 128), torch.zeros(86), cap=cap)
