@@ -50,7 +50,7 @@ RAPID_API int rapid_quantize_rows(const rapid_rows* x, const rapid_rows* q, floa
  *   q, q_scale    as rapid_quantize_rows.  A row with an infinity or NaN: scale NaN, q = 0.
  *   scale, shift  device, bf16, row d (of C elements) at ptr + d*stride; both or neither (NULL: the norm alone)
  *   document      device, int32 [B*n], or NULL; documents: rows of scale and shift, >= 1 (not looked at where document is NULL)
- *   eps           >= 0
+ *   eps           >= 0 and finite
  *   constraints   C a multiple of 8, at most 16384; x, scale, shift 16-byte, q 8-byte aligned, strides multiples of 8; B*n at most 2^22
  * Errors: as rapid_quantize_rows; RAPID_ERR_NULL for scale without shift; RAPID_ERR_ALIAS (q or q_scale begin where an input does).
  */

@@ -365,7 +365,7 @@ int rapid_norm_modulate_int8(const rapid_rows* x, const rapid_rows* q, float* q_
 {
     RowsParams p = {};
     if (!scale != !shift) return RAPID_ERR_NULL;
-    if (!(eps >= 0.f) || (document && documents < 1)) return RAPID_ERR_SHAPE;
+    if (!(eps >= 0.f) || isinf(eps) || (document && documents < 1)) return RAPID_ERR_SHAPE;      // (Newton's step on a root of 0 is no number)
     const int rc = rows_of(x, q, q_scale, B, n, C, 16384, p);
     if (rc != RAPID_OK) return rc;
     const int vectors = document ? documents : B;

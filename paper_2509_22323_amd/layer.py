@@ -136,6 +136,8 @@ class PackedLayer:
         _check_sizes(weights, 1, H, D, image, text, layout, eps, 1, 16)
         if documents < 1:
             raise ValueError(f"{documents} documents: there must be one at least")
+        if not eps < 2.0 ** 128:
+            raise ValueError("eps must be finite in fp32")
         self.H, self.D, self.layout, self.eps, self.axes, self.documents = H, D, layout, eps, axes, documents
         self.tokens = (image, text)
         self.small = [{k: t for k, t in w.items() if k not in self.PRODUCTS} for w in weights]

@@ -4,6 +4,7 @@ import torch
 
 import paper_2509_22323_amd as ra
 from paper_2509_22323_amd import layer as layer_module
+from test_packed_abi import A, ALIGN, SHAPE, norm
 from test_packed_layer import make, no_calls  # noqa: F401
 
 
@@ -24,3 +25,15 @@ def test_caps_of_a_layer(cap, monkeypatch):
     monkeypatch.setattr(layer_module, "_b", None)
     with pytest.raises(ValueError):
         layer.run(torch.zeros(77, 128), torch.zeros(9, 128), torch.zeros(3, 128), torch.zeros(86), cap=cap)
+
+
+def test_a_norm_takes_finite_eps_alone():
+    """1 / sqrt(infinity) by Newton's steps would be NaN, not 0 (an unaligned row: nothing is launched)"""
+    odd = (A + 8, 0, 64)
+    assert norm(eps=float("inf"), x=odd) == SHAPE and norm(eps=3.4e38, x=odd) == ALIGN
+
+
+@pytest.mark.parametrize("eps", [float("inf"), 1e39, float("nan")])
+def test_a_layer_takes_finite_eps_alone(eps):
+    with pytest.raises(ValueError):
+        make(eps=eps)
