@@ -45,7 +45,10 @@ RAPID_API int rapid_quantize_rows(const rapid_rows* x, const rapid_rows* q, floa
  * q, q_scale <- the rows of rapid_quantize_rows of
  *   y = (x[b,r,:] - mean) / sqrt(variance + eps) * (1 + scale[d,:]) + shift[d,:]
  * with d = b, or document[b*n + r] where document is given.  fp64 throughout, y is not rounded in between: q is the formula's, but
- * where the quotient lies within 2^-44 of a border between two integers.  Rows of no document (with document) are left as they were.
+ * where the quotient 127 y / m lies within 2^-43 + 2^-39 R of a border between two integers, R the largest |1 + scale| (|x - mean| +
+ * mean |x|) / sqrt(variance + eps) of the row against the largest |y|.  (1 to 2 for rows about 0, whatever their size; a mean far
+ * above the deviation, or a shift that takes the norm away again, costs as many digits as it is above what is left.)  Rows of no
+ * document (with document) are left as they were.
  *   x             device, bf16, rows [B, n, C]
  *   q, q_scale    as rapid_quantize_rows.  A row with an infinity or NaN: scale NaN, q = 0.
  *   scale, shift  device, bf16, row d (of C elements) at ptr + d*stride; both or neither (NULL: the norm alone)

@@ -211,7 +211,8 @@ __device__ __forceinline__ double larger_of(double a, double b)
 
 // The norm, in fp64: what it ends in are whole numbers, and a result in 32 bits would be on another side of a border between two of them than
 // the formula's about once in 10^5 elements, at another place for every order of the sums.  (The card adds and multiplies as fast
-// in 64 bits as in 32.)  Bound by the vector instructions, 25 an element, 15 of which are the formula's: 8 x 4096 rows of 1536 46.8 us, 3.2 TB/s.
+// in 64 bits as in 32.  Sums here are 58 additions deep at most, which the bound in include/rapid_packed.h counts on.)
+// Bound by the vector instructions, 25 an element, 15 of which are the formula's: 8 x 4096 rows of 1536 46.8 us, 3.2 TB/s.
 // FULL: every access of every lane is one of the row's; the form for any width takes 7 % more instructions.
 template <int WAVES, int CHUNKS, bool FULL>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_rows8_kernel(RowsParams p)
