@@ -46,3 +46,18 @@ def test_codes_are_the_formulas(C, kind):
     assert (np.abs(widen(q)[0] - 127 * y / m[:, None]) <= 0.5 + 2.0 ** -43 + 2.0 ** -39 * R[:, None]).all()
     # (rounded once to fp32, of a maximum that is off by (58 R + 2) u)
     assert (np.abs(widen(q_scale)[0] - m / 127) <= (2.0 ** -24 * (1 + 2.0 ** -20) + 2.0 ** -47 * R) * m / 127).all()
+
+
+@pytest.mark.parametrize("product", [p for p in linear8_plan.PRODUCTS if p[5] > 1], ids=str)
+def test_without_a_workspace(product):
+    """The C entry without one, where the plan would cut the product along K: the same bits"""
+    B, n, K, N, _, _ = product
+    x, w, xs, ws = codes((B, n, K), 1), codes((N, K), 2), scales((B, n), 3, 0.01), scales((N,), 4, 0.01)
+    bias, residual = normal((N,), 5), normal((B, n, N), 7)
+    assert ra.rapid_linear_int8_workspace_bytes(B * n, N, K) > 0
+    want = ra.rapid_linear_int8(x, xs, w, ws, torch.empty((B, n, N), dtype=torch.bfloat16, device="cuda"), bias, "gelu_tanh", None, residual)
+    got = torch.full_like(want, float("nan"))
+    rows = [ra.binding._rows("", t, None, dtype)[0] for t, dtype in ((x, "int8"), (got, "bfloat16"), (residual, "bfloat16"))]
+    status = ra.library().rapid_linear_int8(rows[0], xs.data_ptr(), w.data_ptr(), K, ws.data_ptr(), bias.data_ptr(), rows[1], 2, None, 0, rows[2], None, 0,
+                                            B, n, N, K, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert status == 0 and torch.equal(got.view(torch.int16), want.view(torch.int16))
