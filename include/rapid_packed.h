@@ -90,7 +90,12 @@ RAPID_API size_t rapid_linear_int8_workspace_bytes(long long M, int N, int K);
  *   sees itself, then token by token; 0 for text and 1 for its image: text that does not see the image; the number of a frame: whole
  *   frames one after the other.
  * A token of a document always sees itself; tokens of no document output zeros.  What a token does not see has no part in its
- * output, whatever it holds (infinities and NaN too).
+ * output, whatever it holds (infinities and NaN too; but where another document's values hold one, the rows that share a tile of 64
+ * tokens with it are computed key by key, which takes some hundred times as long).
+ * Arithmetic: as rapid_attn_dense (bf16 matrix products with fp32 sums, weights rounded to bf16 for the second one, the divisor the sum of
+ * the rounded weights); scores, caps and statistics in fp32.  Rows are right wherever their scores are numbers of fp32; one with none
+ * above -7e29 or so is computed key by key.  Range of v: weights are 2^8 at most against the reference of their row, so |v| up to
+ * 2^97 cannot overflow in the sums, whatever the scores; beyond, sums can be infinite where the result is not.
  *   segments  HOST array of n_segments (1 or 2) descriptors as rapid_attn_joint takes them; here n is any number >= 1 in both, and
  *             the segments' strides need not be the same
  *   document  device, int32, that of token t of sample b at document + b*document_stride_b + t (t over the joint sequence)

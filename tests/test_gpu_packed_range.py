@@ -116,3 +116,42 @@ def test_caps_and_scales_that_fp32_holds_as_zero(form, kw):  # noqa: F811
     with pytest.raises(ValueError):
         attend(q, k, v, torch.zeros(100, dtype=torch.int32, device="cuda"), o=o, **kw)
     assert (o == 7.0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [94, -100])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_values_far_from_one(D, power, cap):
+    """|V| up to 2^97 cannot overflow, whatever the scores: of keys whose scores climb a weight is 2^8 at most against its row's reference"""
+    N, lengths = 700, (400, 250)
+    q, k, v = normal((3, 1, 1, N, D), 4)
+    k = torch.linspace(-0.6, 0.6, N, device="cuda")[:, None].expand_as(k) + 0.05 * k.float()
+    q, k, v = q * 0 + 2.0, k.to(q.dtype), v * 2.0 ** power
+    d = np.stack([documents(N, lengths)])
+    got = attend(q, k, v, torch.from_numpy(d).cuda(), cap=cap)
+    o, p = po.attention(widen(q), widen(k), widen(v), d, None, cap)
+    assert_within(got, o, bound(widen(q), widen(k), widen(v), p, o, cap, D ** -0.5, po.visible(d)))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("where", ["k", "v", "both"])
+@pytest.mark.parametrize("value", [NAN, float("inf"), -float("inf"), 3.3895e38])
+def test_what_is_not_visible_has_no_part_under_a_cap(D, where, value):
+    """As without one: infinities and NaN in padding, in other documents and in tokens of a later order, in tiles that others share"""
+    N, bad = 250, [95, 129, 229, 240, 249]
+    d, order = documents(N, (90, 40, 100)), np.arange(N, dtype=np.int32) // 10
+    q, k, v = normal((3, 1, 2, N, D), 5)
+    q *= 3.0
+    clean = [widen(t) for t in (q, k, v)]
+    for t in (k, v):
+        if where in ("both", "k" if t is k else "v"):
+            t[:, :, bad, 3:9] = value
+    got = widen(attend(q, k, v, torch.from_numpy(d).cuda(), torch.from_numpy(order).cuda(), 10.0))
+    see = po.visible(d[None], order[None])
+    fine = ~see[0][:, bad].any(1)
+    assert fine[:90].all() and fine.sum() > 150
+    o, p = po.attention(*clean, d[None], order[None], 10.0)
+    off = bound(*clean, p, o, 10.0, D ** -0.5, see)
+    assert (np.abs(got - o) <= off)[:, :, fine].all()
+    if where == "v" and not np.isfinite(value):
+        assert not np.isfinite(got[:, :, ~fine & (d >= 0)][..., 3:9]).any() and np.isfinite(got[:, :, ~fine][..., 9:]).all()
