@@ -138,6 +138,11 @@ class PackedLayer:
             raise ValueError(f"{documents} documents: there must be one at least")
         if not eps < 2.0 ** 128:
             raise ValueError("eps must be finite in fp32")
+        if H * D > 16384:
+            raise ValueError(f"{H * D} channels: a norm has 16384 at most")
+        for stream, w in zip(("image", "text"), weights):
+            if w["ff_in_w"].shape[0] > 2 ** 17 - 16:
+                raise ValueError(f"{stream} stream: {w['ff_in_w'].shape[0]} channels of the feed-forward block, of which a product in 8 bits takes 2^17 - 16 at most")
         self.H, self.D, self.layout, self.eps, self.axes, self.documents = H, D, layout, eps, axes, documents
         self.tokens = (image, text)
         self.small = [{k: t for k, t in w.items() if k not in self.PRODUCTS} for w in weights]

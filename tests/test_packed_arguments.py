@@ -4,6 +4,7 @@ import torch
 
 import paper_2509_22323_amd as ra
 from paper_2509_22323_amd import layer as layer_module
+from test_joint_layer import weights
 from test_packed_abi import A, ALIGN, SHAPE, norm
 from test_packed_layer import make, no_calls  # noqa: F401
 
@@ -37,3 +38,12 @@ def test_a_norm_takes_finite_eps_alone():
 def test_a_layer_takes_finite_eps_alone(eps):
     with pytest.raises(ValueError):
         make(eps=eps)
+
+
+@pytest.mark.parametrize("kw", [dict(second=dict(F=2 ** 17)), dict(first=dict(F=2 ** 17)), dict(first=dict(F=16, C=257 * 64), second=dict(F=16, C=257 * 64), H=257)], ids=str)
+def test_widths_that_a_run_would_refuse(kw):
+    """A product of 2^17 inputs was refused behind the attention's, that is with the image's states half way"""
+    with torch.device("meta"):
+        streams = [weights(**{"F": 64, **kw.get(name, {})}) for name in ("first", "second")]
+    with pytest.raises(ValueError):
+        make(*streams, H=kw.get("H", 2))
