@@ -182,6 +182,9 @@ class PackedLayer:
             raise ValueError(f"conditioning: {list(conditioning.shape)}, a vector each of 1 to {self.documents} documents")
         if (positions is None) != (self.axes is None):
             raise ValueError("positions: where the layer has axes, and only there")
+        for name, t, n in zip(("image", "text"), (image, text), self.tokens):
+            if tuple(t.shape) != (n, self.H * self.D) or (n > 1 and t.stride(0) < t.shape[1]):
+                raise ValueError(f"{name}: rows [{n}, {self.H * self.D}] that share no element, not {list(t.shape)} with strides {list(t.stride())}")
         for name, t in (("document", document), ("order", order)):
             if t is not None and tuple(t.shape) != (sum(self.tokens),):
                 raise ValueError(f"{name} must be [{sum(self.tokens)}], not {list(t.shape)}")

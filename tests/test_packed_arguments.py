@@ -47,3 +47,14 @@ def test_widths_that_a_run_would_refuse(kw):
         streams = [weights(**{"F": 64, **kw.get(name, {})}) for name in ("first", "second")]
     with pytest.raises(ValueError):
         make(*streams, H=kw.get("H", 2))
+
+
+@pytest.mark.parametrize("kw", [dict(image=torch.zeros(76, 128)), dict(image=torch.zeros(77, 64)), dict(text=torch.zeros(1, 9, 128)), dict(text=torch.zeros(1, 128).expand(9, 128)),
+                                dict(image=torch.zeros(77 * 64 + 64).as_strided((77, 128), (64, 1)))], ids=lambda kw: " ".join(kw))
+def test_states_that_a_run_would_refuse(kw, monkeypatch):
+    """Text whose rows lie upon each other was refused behind the image's last product"""
+    layer = make()
+    monkeypatch.setattr(layer_module, "_b", None)
+    args = dict(image=torch.zeros(77, 128), text=torch.zeros(9, 128), conditioning=torch.zeros(3, 128), document=torch.zeros(86))
+    with pytest.raises(ValueError):
+        layer.run(**{**args, **kw})
