@@ -8,7 +8,8 @@
  *   rapid_norm_modulate_int8  rapid_norm_modulate that ends in such rows
  *   rapid_linear_int8         rapid_linear on them
  * A scale for each token and sums of integers, which are exact in any order, make a row's result independent of what it is packed
- * with: of rapid_quantize_rows, rapid_norm_modulate_int8 and rapid_linear_int8 the same row gives the same bits in every call.
+ * with: of rapid_quantize_rows, rapid_norm_modulate_int8 and rapid_linear_int8 the same row gives the same bits in every call (of the
+ * last but for the sign of zeros).
  *
  * DOCUMENTS.  Where a call takes `document`, it holds a number for each row (token), in any order: rows of equal numbers >= 0 belong
  * together, and where the conditioning's vectors are given they are numbered by it.  -1 (anything below 0): a row of no document,
@@ -72,7 +73,9 @@ RAPID_API int rapid_norm_modulate_int8(const rapid_rows* x, const rapid_rows* q,
  *   constraints  K a multiple of 16, at most 2^17 - 16 (the sums fit 32 bits whatever the integers); x, w 16-byte aligned, their strides
  *             multiples of 16; scales and document 4-byte, y, residual, bias, gate 2-byte aligned; K <= w_stride <= 2^22; N <= 2^22;
  *             B*n < 2^31 - 256.  The rows of two consecutive samples of x (of 256, where n is small) lie within 2^30 elements.
- * The same row of x gives the same bits, in whatever call.
+ * x_scale[b*n + r] times the sum, that times w_scale[j] and what follows are numbers of fp32 each: of scales so far from 1 that one
+ * of them is not, results are infinite or 0.
+ * The same row of x gives the same bits, in whatever call (but for the sign of results that are less than fp32 holds, 0 or -0).
  * Errors: as rapid_linear.
  */
 RAPID_API int rapid_linear_int8(const rapid_rows* x, const float* x_scale, const void* w, long long w_stride, const float* w_scale,

@@ -183,8 +183,9 @@ struct Plan {
 };
 
 // What a product takes, in us, as rapid_linear.hip has it (steps of 128 inputs), fitted to 1200 products of 9 to 32768 rows, 16 to 9728 outputs
-// and 64 to 9728 inputs timed in all tiles and 1 to 8 pieces, inputs changing from call to call: the plan found by it takes 1.006 times
-// what the best one does in the geometric mean (1.22 at most), for 400 others 1.006 (1.18).
+// and 64 to 9728 inputs timed in all tiles and 1 to 8 pieces, inputs changing from call to call, before the epilogue's roundings and the
+// order of its scales were as they are now.  Of the kernels as they are, the plan found by it takes 1.012 times what the best one
+// does in the geometric mean of 250 other products (1.19 at most).
 struct TileCost {
     int rows, columns, slots;
     float alone, full, ends, odd, call, join, sum;

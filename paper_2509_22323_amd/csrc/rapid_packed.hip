@@ -324,6 +324,7 @@ __global__ __launch_bounds__(256) void packed_known_kernel(PackedParams p)
 // units busy half of the cycles each; without the barriers 2 % less time, without exponents 2.5 %.  At D = 64 by the vector instructions, which are the
 // same for half the products: 161 to 170 us (0.85 to 0.81 PFLOP/s).  A cap is seven instructions a score more, where its polynomial serves: 322 to 341 us at
 // D = 128, 234 to 240 at D = 64 (vector units 87 % busy).  Workgroups a CU: two of 230 registers at D = 128, three of 168 at 64.
+// (52 to 64 scalars lie in lanes of vector registers, read back outside the loop but for a few.)
 // 256 queries a workgroup at D = 128: 5 % less time for one document, 5 to 18 % more for documents of a few hundred tokens.  64 queries a
 // wavefront at D = 64 (half the reads of LDS): 10 % more, with two wavefronts a SIMD for three.
 // ---------------------------------------------------------------------------
@@ -877,9 +878,14 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedParams p)
 }
 
 // Into how many pieces the tiles of every group are cut where the groups do not fill the card (a tile of a workgroup that has a CU to itself takes
-// 1.3 us, most of it waiting): as many as make 512 workgroups, of four tiles at least, or 768 of twelve.  us, whole / cut, one head of
+// 1.3 us, most of it waiting): as many as make 512 workgroups, of four tiles at least, or 768 of twelve, of groups that see all of the sequence
+// (the host does not know the documents).  us, whole / cut, one document, one head of
 // 64 1000 tokens 26.9 / 16.2, 8000 172.8 / 43.4; five 4000 92.2 / 42.6, 8000 178.8 / 110.3; two of 128 1000 34.3 / 20.2, 4000 113.2 / 40.9 (into twelve
-// 48.5); eight of 128 2000 63.6 / 41.8 (768 workgroups of five tiles 47.5), 4000 116.0 / 76.0 (512 of 31 tiles 82.8).
+// 48.5); eight of 128 2000 63.6 / 41.8 (768 workgroups of five tiles 47.5), 4000 116.0 / 76.0 (512 of 31 tiles 82.8).  Groups of short
+// documents see few tiles, most of their pieces none, and the parts and the join cost 4 to 25 us more than they save: documents of
+// 128 tokens, 1000 tokens in all, two heads of 64 8.5 / 12.5, of 128 10.7 / 15.4; 8000 16.1 / 30.9, 18.7 / 43.5; documents of 1024 tokens 28.6 / 33.7
+// and 36.1 / 50.7 there, but 21.3 / 15.6 and 28.2 / 19.6 of 1000 in all.  (Pieces without a tile that write nothing and are not joined: 22 to
+// 39 us for documents of 128 among 4608 and 8000 tokens, but one document 3 to 8 % slower.)
 int pieces_for(long long groups, long long tiles)
 {
     constexpr long long MOST = 8;

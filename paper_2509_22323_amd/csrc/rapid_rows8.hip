@@ -81,7 +81,7 @@ __device__ __forceinline__ unsigned bytes(unsigned a, unsigned b, unsigned c, un
     return ab | cd;
 }
 
-// The quotient 127 v / m of a row whose largest magnitude is m, rounded once.  With m = a 2^e, a in [1, 2): t = 127 v 2^-e is exact (15 bits; what
+// The quotient 127 v / m of a row whose largest magnitude is m, rounded once.  With m = a 2^e, a in [0.5, 1): t = 127 v 2^-e is exact (15 bits; what
 // is lost of tiny elements is far below the smallest quotient that does not round to 0), and so is the remainder t - q a of a quotient
 // q = t (1/a) that is off by a step or two; one correction by it gives the quotient rounded to 24 bits, which is a tie between two
 // integers only where the exact one is: v and a have 8 bits each, so any other quotient is 2^-17 or more away from one.
@@ -382,8 +382,9 @@ int rapid_norm_modulate_int8(const rapid_rows* x, const rapid_rows* q, float* q_
     p.documents = documents;
     p.eps = eps;
     p.share = 1.0 / C;
-    // As few wavefronts a row as hold it (joining sums of several costs three barriers a row), with no access that nothing is left for, and four
-    // wavefronts rather than two or eight of a longer one.  us, rows of 1536 by 1 / 2 / 4 wavefronts: 8192 of them 14.1 / 15.7 / 19.2; of 2432 by
+    // As few wavefronts a row as hold it (joining sums of several costs three barriers a row) in a form that there is: five accesses take that of
+    // six, seven that of eight over two wavefronts, where the last access of every lane, or of one wavefront, is empty (forms of five and
+    // seven have not been measured); and four wavefronts rather than two or eight of a longer row.  us, rows of 1536 by 1 / 2 / 4 wavefronts: 8192 of them 14.1 / 15.7 / 19.2; of 2432 by
     // 1 x 6, 2 x 3, 4 x 2 accesses 21.1 / 21.7 / 25.8 (2 x 4: 23.9); of 6144 by 2 x 6, 4 x 3, 4 x 4, 8 x 2 51.4 / 47.5 / 52.5 / 55.6; 4096
     // of 9728 by 4 x 6, 8 x 3, 8 x 4 42.7 / 47.6 / 51.7.  A few hundred rows take 5.3 to 6.3 us by any.
     const int accesses = (C + 511) / 512;              // of a wavefront

@@ -141,7 +141,8 @@ typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
 // 1 KB from 64 lanes' addresses into LDS: lane i's 16 bytes go to dst + 1024 C + 16 i.  (The instruction's offset counts on both
 // sides: LESS is taken off the lanes' offsets.)  Assembly, so that only the waits below order it; a wait state between the scalar
-// write of M0 and the copy.
+// write of M0 and the copy.  It would take five behind a vector instruction that writes the descriptor or the offset, as one that reads a
+// scalar back from a lane does: the compiler has none there, which tests/test_wait_states.py looks at before anything runs.
 constexpr unsigned LESS = 3 * 1024;
 template <int C>
 __device__ __forceinline__ void copy_1k(const i32x4& buffer, unsigned off, int at, unsigned dst)

@@ -88,6 +88,9 @@ __device__ __forceinline__ bf16x8 finished(const P& p, float (&z)[8], bf16x8 gat
 // orders of tiles (GROUP 2, 6, 8, 16), weights past the caches, touching the next steps in the L2 first, 128 x 64 outputs a wavefront
 // with four wavefronts, all copies in a step's first half, priorities of waves, five steps in LDS for the small tiles: none faster over
 // products of 64 to 8192 rows, most 1 to 20 % slower.
+// The ends of tiles keep lane masks of all their units at once, of which some go to lanes of vector registers and back: 8 to 31 scalars in bf16
+// (435 v_readlane among 14416 instructions at 128 x 128), 18 to 113 in 8 bits, but 596 at 128 x 128, with 7160 v_readlane among 23139
+// instructions: tiles that end slower than they could.
 // Of 8-bit integers, 128 inputs a step, the same copies feed twice the products: 8192 x 8192 x 8192 405 us (2.72 P/s; the matrix library's
 // plain product 450), 9728 -> 2432 with gate and residual 195 to 203 us, pipe busy 57 %, 1536 -> 4608 60 to 66, 47 %: twelve steps a tile, then
 // scales, bias and 75 MB of results.

@@ -1,4 +1,4 @@
-"""Host-only checks of arguments that fp32 does not hold as they are; no GPU needed."""
+"""Host-only checks of what calls on packed sequences refuse: numbers that fp32 does not hold, and what a layer would refuse half way."""
 import pytest
 import torch
 
