@@ -69,7 +69,7 @@ typedef enum {
  * The same call gives the same bits, whenever it is made.  The order in which a sum's K terms are added is another for other sizes,
  * with or without a workspace, and in other tiles of one product: equal rows of x, in one call or in calls of other sizes, can
  * give outputs that differ by what fp32 sums in another order differ by.  Products of up to four rows (B*n <= 4) need no workspace, and
- * there the sums of a row, and its outputs without gate and residual, are the same bits in whatever call of as many rows.
+ * there the sums of a row, and its outputs without gate and residual, are the same bits in whatever call of up to four rows.
  * y shares no byte with x, w, bias or gate, and none with residual but as above.
  * Errors: RAPID_ERR_NULL; RAPID_ERR_SHAPE (sizes, strides); RAPID_ERR_UNSUPPORTED (K % 8, activation); RAPID_ERR_ALIGN;
  * RAPID_ERR_WORKSPACE (given, but too small or not aligned); RAPID_ERR_ALIAS (y starts where x, w, bias or gate does, or where

@@ -315,7 +315,9 @@ __global__ __launch_bounds__(256) void packed_known_kernel(PackedParams p)
 // The kernel: a workgroup takes 128 queries of a head, a wavefront 32 of them, and goes over the tiles that one of them sees.
 // S^T = K Q^T, one query a lane, and O^T += V^T P^T, v_mfma_f32_16x16x32_bf16; P goes from one product to the next in registers, and
 // o = sum p v / sum p with p = 2^(x - m), x the exponents and m a reference that only moves when one is 2^8 above it, so that
-// accumulators are rescaled a few times a row.  p is rounded to bf16 for the product, and the sum is of the rounded values.
+// accumulators are rescaled a few times a row.  p is rounded to bf16 for the product, whose operands have as many bits as V has, and the sum is
+// of the rounded values, so that no row's weights add up to another number than 1: outputs are 0.0020 to 0.0023 of their size off the exact ones in
+// the mean square, of which their own rounding to bf16 is 0.0017.
 // Tiles that every query sees whole take no mask at all; others compare the documents and orders that were copied beside their values.
 //
 // Two tiles of keys and two of values in LDS, copied past the registers a whole step ahead, one barrier a step; in a step the scores of the
@@ -884,8 +886,9 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedParams p)
 // 48.5); eight of 128 2000 63.6 / 41.8 (768 workgroups of five tiles 47.5), 4000 116.0 / 76.0 (512 of 31 tiles 82.8).  Groups of short
 // documents see few tiles, most of their pieces none, and the parts and the join cost 4 to 25 us more than they save: documents of
 // 128 tokens, 1000 tokens in all, two heads of 64 8.5 / 12.5, of 128 10.7 / 15.4; 8000 16.1 / 30.9, 18.7 / 43.5; documents of 1024 tokens 28.6 / 33.7
-// and 36.1 / 50.7 there, but 21.3 / 15.6 and 28.2 / 19.6 of 1000 in all.  (Pieces without a tile that write nothing and are not joined: 22 to
-// 39 us for documents of 128 among 4608 and 8000 tokens, but one document 3 to 8 % slower.)
+// and 36.1 / 50.7 there, but 21.3 / 15.6 and 28.2 / 19.6 of 1000 in all.  (Pieces of four tiles that the
+// group sees, the others not written and not joined, on another card: 22 to 39 us for documents of 128 tokens among 4608 and 8000, but 12.5 became
+// 13.4 and 15.4 15.8, and one document takes 3 to 8 % more.)
 int pieces_for(long long groups, long long tiles)
 {
     constexpr long long MOST = 8;

@@ -19,6 +19,7 @@ WEIGHTS = ("mod_w", "mod_b",           # [6C, C]: shift, scale, gate of the atte
            "ff_out_w", "ff_out_b")     # [C, F]
 
 
+MOST = (2 - 2.0 ** -23) * 2.0 ** 127   # of fp32
 _NONE_ALLOWED = ("mod_b", "qkv_b", "q_norm", "k_norm", "out_b", "ff_in_b", "ff_out_b")
 
 
@@ -136,7 +137,7 @@ class PackedLayer:
         _check_sizes(weights, 1, H, D, image, text, layout, eps, 1, 16)
         if documents < 1:
             raise ValueError(f"{documents} documents: there must be one at least")
-        if not eps < 2.0 ** 128:
+        if not eps <= MOST:
             raise ValueError("eps must be finite in fp32")
         if H * D > 16384:
             raise ValueError(f"{H * D} channels: a norm has 16384 at most")
@@ -188,7 +189,7 @@ class PackedLayer:
         for name, t in (("document", document), ("order", order)):
             if t is not None and tuple(t.shape) != (sum(self.tokens),):
                 raise ValueError(f"{name} must be [{sum(self.tokens)}], not {list(t.shape)}")
-        if not (cap == 0 or 2.0 ** -149 <= cap < 2.0 ** 128):
+        if not (cap == 0 or 2.0 ** -149 <= cap <= MOST):
             raise ValueError("cap must be 0 or a positive number of fp32")
         import torch
         if torch._C._cuda_getDevice() == self.device:

@@ -20,7 +20,7 @@ def test_caps_and_scales_that_fp32_holds_as_zero(kw):
         ra.rapid_attn_packed([(q, q, q, q)], torch.zeros(4, dtype=torch.int32), cap=1e-44, scale=1e-44)
 
 
-@pytest.mark.parametrize("cap", [1e-46, 4e38])
+@pytest.mark.parametrize("cap", [1e-46, 4e38, 3.4028235677973366e38])
 def test_caps_of_a_layer(cap, monkeypatch):
     layer = make()
     monkeypatch.setattr(layer_module, "_b", None)
@@ -34,7 +34,7 @@ def test_a_norm_takes_finite_eps_alone():
     assert norm(eps=float("inf"), x=odd) == SHAPE and norm(eps=3.4e38, x=odd) == ALIGN
 
 
-@pytest.mark.parametrize("eps", [float("inf"), 1e39, float("nan")])
+@pytest.mark.parametrize("eps", [float("inf"), 1e39, 3.4028235677973366e38, float("nan")])
 def test_a_layer_takes_finite_eps_alone(eps):
     with pytest.raises(ValueError):
         make(eps=eps)
