@@ -124,8 +124,8 @@ class PackedLayer:
     time, whose sums are each request's own; what a token comes to does not depend on what it is packed with, but for the order in
     which its attention's sums are added.
 
-    weights as JointLayer takes them; those of the projections are quantised here, on the current stream, and not kept: a run on another
-    stream waits for that one first, as with any tensor.  Its buffers serve one run at a time.  image, text: tokens that the
+    weights as JointLayer takes them; those of the projections are quantised here, on the current stream, and not kept: a run on
+    another stream has to wait for that one first, as with any tensor.  Its buffers serve one run at a time.  image, text: tokens that the
     tensors of a run have, any numbers; documents: how many requests a run holds at most; axes (RopeAxis each): the rotation of
     queries and keys, None = none.  F is a multiple of 16."""
 
