@@ -45,3 +45,32 @@ def test_requests_up_to_their_attention(H, D):
     for first, count in ((0, 1), (7, 1), (11, 1), (3, 2), (1, 4), (0, 5), (4, 5), (2, 8), (0, 9), (3, 9)):
         for got, want in zip(run(first, count), whole):
             assert same(got, want[first:first + count]), (first, count)
+
+
+def test_nine_requests_in_a_graph():
+    """Three calls a stream for their conditioning; replays between eager runs, on other conditioning each time"""
+    count, H, D = 9, 3, 64
+    joint = make_joint(H=H, D=D, F=16, rotate=False)[0]
+    layer = ra.PackedLayer(joint.weights, H, D, 3 * count, 2 * count, count)
+    start = [normal((n * count, H * D), 6 + n, 2.0) for n in (3, 2)]
+    hidden, cond = [t.clone() for t in start], normal((count, H * D), 5)
+    document = torch.cat([torch.arange(count, device="cuda", dtype=torch.int32).repeat_interleave(n) for n in (3, 2)])
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        layer.run(*hidden, cond, document)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.run(*hidden, cond, document)
+    for turn in range(3):
+        cond.copy_(normal((count, H * D), 20 + turn))
+        for t, s in zip(hidden, start):
+            t.copy_(s)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in hidden]
+        for t, s in zip(hidden, start):
+            t.copy_(s)
+        layer.run(*hidden, cond, document)
+        assert all(same(a, b) for a, b in zip(got, hidden)) and not same(hidden[0], start[0])
